@@ -266,6 +266,85 @@ int mixaq_downsample_forward(const mixaq_downsample *h, const float *x, float *y
 int mixaq_downsample_forward_taps(const mixaq_downsample *h, const float *x, float *y, void *stream,
                                   int8_t *tap_codes, int32_t *tap_acc);
 
+/* ---- linear layers in 8-bit float, and the norms between them --------------------------------- */
+
+/* The layers that a model has around its two-branch blocks (neck, decoder, head, blocks that are left uncalibrated), in 8 bits
+ * without calibration: codes are 8-bit floats (e4m3: sign, 4 exponent and 3 fraction bits, largest value 448, no infinity)
+ * and every block of 128 columns has a scale of its own, taken from the values.  Outside the paper's method.
+ *
+ * A matrix of rows (tokens), in device memory.  Row r starts at data + r * stride; of a block of 128 columns b (the last one may be
+ * shorter) row r's scale is scales[b * scale_stride + r], and the values that codes stand for are code * scale.  Values may
+ * start at any multiple of their size and have any stride >= columns.  Codes and their stride are multiples of 16 bytes, and every row
+ * (the last one too) has room for its columns rounded up to 16: those bytes are read, what they hold changes nothing, and they are never
+ * written. */
+typedef enum { MIXAQ_F32 = 0, MIXAQ_F16 = 1, MIXAQ_BF16 = 2, MIXAQ_E4M3 = 3 } mixaq_type;
+typedef struct {
+    void    *data;
+    int64_t  stride;          /* elements from one row to the next                                 */
+    int32_t  type;            /* mixaq_type                                                        */
+    float   *scales;          /* MIXAQ_E4M3 only                                                   */
+    int64_t  scale_stride;    /* MIXAQ_E4M3 only: floats from one block of columns to the next     */
+} mixaq_rows;
+
+/* Values to codes: of every block of block_rows x 128 values (block_rows 1: activations, 128: weights)
+ *   scale = max(largest |v|, 2^-100) / 448,  code = e4m3(v * (1/scale)),
+ * quotient, inverse and product rounded to binary32, the code to the nearest value (ties to even), at most 448 in size.  A
+ * block that holds a NaN or an infinity gets the scale NaN and codes NaN.  With block_rows 128, rows r .. r+127 share the scale
+ * scales[b * scale_stride + r / 128].  x: values; q: codes; they must not overlap.  rows may be 0. */
+int mixaq_scaled_quantize(const mixaq_rows *x, int32_t rows, int32_t columns, int32_t block_rows, const mixaq_rows *q, void *stream);
+
+/* y = act(x w^T + bias): on codes of x [rows, K] and of w [N, K].  Of each block of 128 columns the exact products are summed, then one fused
+ * multiply-add with the product of the two scales takes the sum to the others; one rounding to y's type at the end.  Sums are binary32; for
+ * a y of 16 bits the sum of a block is that of the 8-bit matrix instruction, which keeps 14 bits of eight neighbouring products, counted
+ * from the largest of them.  x may be given as values: they are quantized first, as mixaq_scaled_quantize with block_rows 1 does, with the same
+ * result.  y may be codes: the binary32 results are quantized, as mixaq_scaled_quantize does. */
+typedef struct {
+    int32_t K, N;             /* inputs and outputs per row: 1 .. 65536                           */
+    int32_t activation;       /* 0: none, 1: GELU (erf form)                                      */
+} mixaq_scaled_linear_desc;
+typedef struct {
+    mixaq_rows   w;           /* MIXAQ_E4M3, [N][K], scales as of mixaq_scaled_quantize with block_rows 128 */
+    const float *bias;        /* device [N] or NULL                                               */
+} mixaq_scaled_linear_params;
+typedef struct mixaq_scaled_linear mixaq_scaled_linear;
+
+/* Packs the parameters into library-owned device memory in the order that the matrix instruction takes them; the caller's
+ * buffers may be released afterwards.  Synchronises `stream` once before returning. */
+int mixaq_scaled_linear_create(const mixaq_scaled_linear_desc *desc, const mixaq_scaled_linear_params *params, void *stream,
+                               mixaq_scaled_linear **out);
+int mixaq_scaled_linear_destroy(mixaq_scaled_linear *h);
+/* Bytes of device workspace that mixaq_scaled_linear_forward needs for up to `rows` rows of these types (0: none, workspace may be
+ * NULL); a workspace is 256-byte aligned.  Calls that may overlap in time need workspaces of their own, captured ones included. */
+int mixaq_scaled_linear_workspace_bytes(const mixaq_scaled_linear *h, int32_t rows, int32_t x_type, int32_t y_type, size_t *bytes);
+/* Allocates nothing and does not wait; may be captured.  x, y and workspace must not overlap.  rows may be 0.  The handle is not
+ * changed: calls on any streams of its device may share it. */
+int mixaq_scaled_linear_forward(const mixaq_scaled_linear *h, const mixaq_rows *x, int32_t rows, const mixaq_rows *y, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* What stands between two layers of a residual stream, in one pass:
+ *   y   = residual_scale * x + gate * post_norm(branch)
+ *   out = pre_norm(y)
+ * in binary32; out takes y before y is rounded to its type.  A norm is 0: none, 1: LayerNorm (biased variance), 2: RMS norm, with
+ * gamma (NULL: 1) and beta (NULL: 0).  gate: one vector for every rows_per_gate rows, [ceil(rows / rows_per_gate)][C] (a vector
+ * per channel: rows_per_gate >= rows; per image: its rows), NULL: 1.  All vectors: device float. */
+typedef struct {
+    int32_t C;                        /* values per row: 1 .. 16384                               */
+    int32_t post_norm, pre_norm;      /* 0, 1, 2                                                  */
+    int32_t rows_per_gate;            /* >= 1; any value without a gate                           */
+    float   post_eps, pre_eps;        /* > 0 where there is a norm                                */
+    float   residual_scale;
+} mixaq_residual_norm_desc;
+typedef struct {
+    const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;      /* [C] or NULL               */
+    const float *gate;
+} mixaq_residual_norm_params;
+/* x: values.  branch: values, or NULL (y = residual_scale * x; then no post_norm and no gate).  y: values of x's type, or NULL.  out:
+ * values, or codes as mixaq_scaled_quantize with block_rows 1 makes them of the binary32 results, or NULL (then no pre_norm); one
+ * of y and out is given.  y or out may be x or branch itself (same data, stride and type); apart from that the outputs overlap
+ * neither the inputs nor each other.  One kernel, allocates nothing.  rows may be 0. */
+int mixaq_residual_norm(const mixaq_residual_norm_desc *desc, const mixaq_residual_norm_params *params, const mixaq_rows *x,
+                        const mixaq_rows *branch, const mixaq_rows *y, const mixaq_rows *out, int32_t rows, void *stream);
+
 /* ---- host-only helpers (no GPU work) ------------------------------------------------------- */
 
 /* Equivalent activation bits (appendix "Calculation of Equivalent Activation Bits"):

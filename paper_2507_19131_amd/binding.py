@@ -60,6 +60,32 @@ class DownsampleParams(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w", "s_w", "bias", "ln_gamma", "ln_beta")] + [("a_in", QParam)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32), ("scales", C.c_void_p), ("scale_stride", C.c_int64)]
+
+
+class ScaledLinearDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("K", "N", "activation")]
+
+
+class ScaledLinearParams(C.Structure):
+    _fields_ = [("w", Rows), ("bias", C.c_void_p)]
+
+
+class ResidualNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("C", "post_norm", "pre_norm", "rows_per_gate")] + \
+               [(n, C.c_float) for n in ("post_eps", "pre_eps", "residual_scale")]
+
+
+class ResidualNormParams(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("post_gamma", "post_beta", "pre_gamma", "pre_beta", "gate")]
+
+
+ROW_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
+ACTIVATIONS = {"none": 0, "gelu": 1}
+NORMS = {"none": 0, "layer": 1, "rms": 2}
+
+
 def lib_path():
     return _LIB_PATH
 
@@ -97,6 +123,13 @@ def load():
         L.mixaq_downsample_destroy.argtypes = [C.c_void_p]
         L.mixaq_downsample_forward.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         L.mixaq_downsample_forward_taps.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.mixaq_scaled_quantize.argtypes = [C.POINTER(Rows), C.c_int32, C.c_int32, C.c_int32, C.POINTER(Rows), C.c_void_p]
+        L.mixaq_scaled_linear_create.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p)]
+        L.mixaq_scaled_linear_destroy.argtypes = [C.c_void_p]
+        L.mixaq_scaled_linear_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.mixaq_scaled_linear_forward.argtypes = [C.c_void_p, C.POINTER(Rows), C.c_int32, C.POINTER(Rows), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mixaq_residual_norm.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows),
+                                          C.c_int32, C.c_void_p]
         L.mixaq_block_set_fused.argtypes = [C.c_void_p, C.c_int32]
         L.mixaq_kernel_name.restype = C.c_char_p
         L.mixaq_kernel_name.argtypes = [C.c_int32]
@@ -325,7 +358,144 @@ def downsample_to_device(inp, device="cuda:0"):
     return bag
 
 
+# ---------------------------------------------------------------- linear layers in 8-bit float, norms between them
+def _rows(t, name, scales=None, block_rows=1):
+    """A 2-D tensor on the current device as a mixaq_rows; a float8_e4m3fn one comes with its scales, float [blocks of 128 columns, rows]
+    (with block_rows 128: [.., blocks of rows])."""
+    if t is None:
+        return None
+    kind = ROW_TYPES.get(t.dtype)
+    if kind is None or t.dim() != 2:
+        raise ValueError("%s must be a 2-D tensor of float32, float16, bfloat16 or float8_e4m3fn" % name)
+    rows, cols = t.shape
+    row, col = t.stride()
+    if col != 1 and cols > 1:
+        raise ValueError("%s: the values of a row must be adjacent (strides %d, %d)" % (name, row, col))
+    _on_device(t, name)
+    if rows < 2:                                          # the stride of a single row means nothing
+        row = -(-cols // 16) * 16
+    if kind != 3:
+        if scales is not None:
+            raise ValueError("%s is not float8_e4m3fn, but scales are given" % name)
+        return Rows(t.data_ptr(), row, kind, None, 0)
+    if scales is None:
+        raise ValueError("%s is float8_e4m3fn: its scales are missing" % name)
+    _vector(scales, name + "'s scales", (-(-cols // 128), -(-rows // block_rows)), strided=True)
+    return Rows(t.data_ptr(), row, kind, scales.data_ptr(), scales.stride(0) if scales.shape[0] > 1 else max(scales.shape[1], 1))
+
+
+def _on_device(t, name):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s must be on the current device (it is on %s)" % (name, t.device))
+
+
+def _vector(t, name, shape, strided=False):
+    """Checks a float tensor of parameters or scales: contiguous, or with `strided` contiguous rows."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be float32 of shape %s (got %s, %s)" % (name, tuple(shape), t.dtype, tuple(t.shape)))
+    if not (t.is_contiguous() or (strided and (t.shape[1] <= 1 or t.stride(1) == 1))):
+        raise ValueError("%s must be contiguous" % name)
+    _on_device(t, name)
+    return t
+
+
+def mixaq_scaled_quantize(x, codes, scales, block_rows=1, stream=None):
+    """x [rows, cols] values -> codes float8_e4m3fn [rows, cols], scales float [ceil(cols / 128), ceil(rows / block_rows)]."""
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128 (got %r)" % (block_rows,))
+    if tuple(codes.shape) != tuple(x.shape):
+        raise ValueError("codes have the shape %s, x %s" % (tuple(codes.shape), tuple(x.shape)))
+    a, q = _rows(x, "x"), _rows(codes, "codes", scales, block_rows)
+    _check(load().mixaq_scaled_quantize(a, x.shape[0], x.shape[1], block_rows, q, _stream(stream)))
+    return codes, scales
+
+
+def mixaq_scaled_linear_create(w, s_w, bias=None, activation="none", stream=None):
+    """w: float8_e4m3fn [N, K], s_w: float [ceil(K / 128), ceil(N / 128)] as of mixaq_scaled_quantize with block_rows 128; bias: float [N]
+    or None; activation: "none" or "gelu".  Returns an opaque handle; w, s_w and bias may be released."""
+    p = ScaledLinearParams(_rows(w, "w", s_w, 128), _ptr(_vector(bias, "bias", (w.shape[0],))))
+    d = ScaledLinearDesc(w.shape[1], w.shape[0], ACTIVATIONS[activation])
+    out = C.c_void_p()
+    _check(load().mixaq_scaled_linear_create(C.byref(d), C.byref(p), _stream(stream), C.byref(out)))
+    out.K, out.N = w.shape[1], w.shape[0]
+    return out
+
+
+def mixaq_scaled_linear_destroy(h):
+    _check(load().mixaq_scaled_linear_destroy(h))
+
+
+def mixaq_scaled_linear_workspace_bytes(h, rows, x_dtype, y_dtype):
+    n = C.c_size_t()
+    _check(load().mixaq_scaled_linear_workspace_bytes(h, rows, ROW_TYPES[x_dtype], ROW_TYPES[y_dtype], C.byref(n)))
+    return n.value
+
+
+def mixaq_scaled_linear_forward(h, x, y, x_scales=None, y_scales=None, workspace=None, stream=None):
+    """x [rows, K] -> y [rows, N]; each of them values, or float8_e4m3fn with its scales."""
+    rows = x.shape[0]
+    if x.shape[1:] != (h.K,) or y.shape != (rows, h.N):
+        raise ValueError("x %s, y %s do not fit a layer of %d inputs and %d outputs" % (tuple(x.shape), tuple(y.shape), h.K, h.N))
+    a, b = _rows(x, "x", x_scales), _rows(y, "y", y_scales)
+    ws, n = None, 0
+    if workspace is not None:
+        _on_device(workspace, "workspace")
+        ws, n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(load().mixaq_scaled_linear_forward(h, a, rows, b, ws, n, _stream(stream)))
+    return y
+
+
+class ResidualNorm:
+    """What mixaq_residual_norm takes besides the rows; keeps its vectors alive."""
+
+    def __init__(self, desc, params, vectors, gates):
+        self.desc, self.params, self.vectors, self.gates = desc, params, vectors, gates
+
+
+def make_residual_norm(channels, post="none", pre="layer", eps=1e-5, residual_scale=1.0, post_gamma=None, post_beta=None, pre_gamma=None,
+                       pre_beta=None, gate=None, rows_per_gate=None):
+    """post, pre: "none", "layer" or "rms"; gammas and betas: float [C] or None; gate: float [C] for all rows, or [G, C] with a vector for
+    every rows_per_gate rows."""
+    if gate is not None:
+        gate = gate.unsqueeze(0) if gate.dim() == 1 else gate
+        if rows_per_gate is None and gate.shape[0] != 1:
+            raise ValueError("gate has %d rows: rows_per_gate is missing" % gate.shape[0])
+        _vector(gate, "gate", (gate.shape[0], channels))
+    vectors = [_vector(v, n, (channels,)) for v, n in ((post_gamma, "post_gamma"), (post_beta, "post_beta"), (pre_gamma, "pre_gamma"),
+                                                       (pre_beta, "pre_beta"))] + [gate]
+    span = 2**31 - 1 if rows_per_gate is None else int(rows_per_gate)
+    desc = ResidualNormDesc(channels, NORMS[post], NORMS[pre], span, eps, eps, residual_scale)
+    return ResidualNorm(desc, ResidualNormParams(*[_ptr(v) for v in vectors]), vectors, None if gate is None else gate.shape[0])
+
+
+def mixaq_residual_norm(norm, x, branch=None, y=None, out=None, out_scales=None, stream=None):
+    """y = residual_scale * x + gate * post(branch), out = pre(y); all [rows, C], y or out may be None (not stored)."""
+    rows = x.shape[0]
+    for t, n in ((x, "x"), (branch, "branch"), (y, "y"), (out, "out")):
+        if t is not None and t.shape != (rows, norm.desc.C):
+            raise ValueError("%s has the shape %s, not (%d, %d)" % (n, tuple(t.shape), rows, norm.desc.C))
+    if norm.gates is not None and rows > norm.gates * norm.desc.rows_per_gate:
+        raise ValueError("%d rows need more than the %d gate vectors of %d rows each" % (rows, norm.gates, norm.desc.rows_per_gate))
+    _check(load().mixaq_residual_norm(C.byref(norm.desc), C.byref(norm.params), _rows(x, "x"), _rows(branch, "branch"), _rows(y, "y"),
+                                      _rows(out, "out", out_scales), rows, _stream(stream)))
+    return y, out
+
+
 # ---------------------------------------------------------------- memory helpers (no arithmetic)
+def alloc_codes(rows, cols, block_rows=1, device="cuda:0"):
+    """Room for codes whose rows start at multiples of 16 bytes, and for their scales."""
+    codes = torch.zeros((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)[:, :cols]
+    return codes, torch.empty((-(-cols // 128), -(-rows // block_rows)), dtype=torch.float32, device=device)
+
+
+def alloc_linear_workspace(h, rows, x_dtype, y_dtype, device="cuda:0"):
+    """None where the call needs none."""
+    n = mixaq_scaled_linear_workspace_bytes(h, rows, x_dtype, y_dtype)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
 class _Bag:
     pass
 

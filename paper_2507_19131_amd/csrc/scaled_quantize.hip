@@ -1,0 +1,167 @@
+// Values to 8-bit float codes with one scale per block of 1 x 128 or 128 x 128 values, and the checks of matrices of rows.
+#include "scaled.h"
+
+#include <algorithm>
+
+using namespace mixaq;
+
+namespace mixaq {
+
+#define HIP_TRY(expr)                                                                                   \
+    do {                                                                                                \
+        hipError_t e_ = (expr);                                                                         \
+        if (e_ != hipSuccess) return fail(MIXAQ_E_HIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
+    } while (0)
+
+int check_rows(const mixaq_rows* m, const char* name, int32_t columns, bool codes_allowed, int32_t scale_rows)
+{
+    if (!m || !m->data) return fail(MIXAQ_E_NULL, "%s is NULL", name);
+    if (m->type < MIXAQ_F32 || m->type > MIXAQ_E4M3) return fail(MIXAQ_E_SHAPE, "%s: unknown type %d", name, m->type);
+    if (m->type == MIXAQ_E4M3 && !codes_allowed) return fail(MIXAQ_E_SHAPE, "%s must be values", name);
+    if (m->stride < columns) return fail(MIXAQ_E_SHAPE, "%s: stride %lld of %d columns", name, (long long)m->stride, columns);
+    if (m->stride > (1LL << 40)) return fail(MIXAQ_E_SHAPE, "%s: stride %lld is too large", name, (long long)m->stride);
+    if ((uintptr_t)m->data % size_of(m->type)) return fail(MIXAQ_E_SHAPE, "%s is not aligned to its values", name);
+    if (m->type == MIXAQ_E4M3) {
+        if (!m->scales) return fail(MIXAQ_E_NULL, "%s: scales is NULL", name);
+        if ((uintptr_t)m->scales % 4) return fail(MIXAQ_E_SHAPE, "%s: scales are not aligned", name);
+        if ((uintptr_t)m->data % 16 || m->stride % 16)
+            return fail(MIXAQ_E_SHAPE, "%s: codes and their stride must be multiples of 16 bytes (stride %lld)", name, (long long)m->stride);
+        if (m->scale_stride < scale_rows || m->scale_stride > (1LL << 40))
+            return fail(MIXAQ_E_SHAPE, "%s: scale_stride %lld of %d rows", name, (long long)m->scale_stride, scale_rows);
+    }
+    return MIXAQ_OK;
+}
+
+bool rows_overlap(const mixaq_rows& a, int32_t rows_a, int32_t columns_a, const mixaq_rows& b, int32_t rows_b, int32_t columns_b)
+{
+    const long long pa = (long long)(uintptr_t)a.data, pb = (long long)(uintptr_t)b.data;
+    const long long sa = a.stride * size_of(a.type), sb = b.stride * size_of(b.type);
+    const long long wa = (long long)columns_a * size_of(a.type), wb = (long long)columns_b * size_of(b.type);
+    if (pa + (rows_a - 1) * sa + wa <= pb || pb + (rows_b - 1) * sb + wb <= pa) return false;
+    if (sa == sb) {                                       // two column ranges of one matrix
+        const long long d = ((pb - pa) % sa + sa) % sa;   // b's first column behind a's
+        if (d >= wa && d + wb <= sa) return false;
+    }
+    return true;
+}
+
+}  // namespace mixaq
+
+namespace {
+
+struct QuantArgs {
+    const void* x;
+    long long ldx;
+    uint8_t* codes;
+    long long ldc;
+    float* scales;
+    long long lds;
+    int rows, cols, nb, units;        // units: groups of 16 rows x blocks of columns
+    FastDiv by_nb;
+};
+
+// One block of a row is 16 lanes with eight values each; a wave takes 16 rows of one block of columns, four at a time, and the waves
+// beside it the next blocks of the same rows.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs A)
+{
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+    for (int u = blockIdx.x * 4 + (threadIdx.x >> 6); u < A.units; u += gridDim.x * 4) {
+        const int rg = A.by_nb(u), b = u - rg * A.nb;
+        const int col = b * SBLOCK + l * 8, n = A.cols - col;
+        float v[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = rg * 16 + j * 4 + g;
+            load8((const T*)A.x + (long long)min(row, A.rows - 1) * A.ldx + col, n, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = rg * 16 + j * 4 + g;
+            const BlockScale s = block_scale(max16(max_magnitude(v[j])));
+            if (row < A.rows) {
+                if (n > 0) store_codes8(A.codes + (long long)row * A.ldc + col, n, v[j], s.inv);
+                if (l == 0) A.scales[b * A.lds + row] = s.scale;
+            }
+        }
+    }
+}
+
+// A workgroup per 128 x 128 tile, held in registers between its maximum and its codes.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_tiles_kernel(QuantArgs A)
+{
+    __shared__ unsigned part[4];
+    const int tr = A.by_nb(blockIdx.x), b = blockIdx.x - tr * A.nb;
+    const int l = threadIdx.x & 15, g = threadIdx.x >> 4, col = b * SBLOCK + l * 8, n = A.cols - col;
+    float v[8][8];
+    unsigned m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int row = tr * SBLOCK + j * 16 + g;
+        load8((const T*)A.x + (long long)min(row, A.rows - 1) * A.ldx + col, n, v[j]);
+        if (row < A.rows) m = max(m, max_magnitude(v[j]));
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    const BlockScale s = block_scale(max(max(part[0], part[1]), max(part[2], part[3])));
+    if (threadIdx.x == 0) A.scales[b * A.lds + tr] = s.scale;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int row = tr * SBLOCK + j * 16 + g;
+        if (row < A.rows && n > 0) store_codes8(A.codes + (long long)row * A.ldc + col, n, v[j], s.inv);
+    }
+}
+
+template <int TYPE>
+void launch(const QuantArgs& A, int block_rows, hipStream_t st)
+{
+    using T = typename TypeOf<TYPE>::T;
+    if (block_rows == 1) hipLaunchKernelGGL(quantize_rows_kernel<T>, dim3(std::min((A.units + 3) / 4, 1 << 22)), dim3(256), 0, st, A);
+    else hipLaunchKernelGGL(quantize_tiles_kernel<T>, dim3(A.units), dim3(256), 0, st, A);
+}
+
+}  // namespace
+
+namespace mixaq {
+
+int launch_quantize(const mixaq_rows& x, int32_t rows, int32_t columns, int32_t block_rows, const mixaq_rows& q, hipStream_t st)
+{
+    QuantArgs A;
+    A.x = x.data; A.ldx = x.stride;
+    A.codes = (uint8_t*)q.data; A.ldc = q.stride;
+    A.scales = q.scales; A.lds = q.scale_stride;
+    A.rows = rows; A.cols = columns; A.nb = blocks_of(columns);
+    const int per = block_rows == 1 ? 16 : SBLOCK;
+    const long long units = ((long long)rows + per - 1) / per * A.nb;
+    if (units >= (1LL << 30) || (block_rows > 1 && units * 256 >= MOST_THREADS))
+        return fail(MIXAQ_E_SHAPE, "%d rows of %d columns are too many for one call", rows, columns);
+    A.units = (int)units;
+    A.by_nb = FastDiv(A.nb);
+    switch (x.type) {
+    case MIXAQ_F32: launch<MIXAQ_F32>(A, block_rows, st); break;
+    case MIXAQ_F16: launch<MIXAQ_F16>(A, block_rows, st); break;
+    default: launch<MIXAQ_BF16>(A, block_rows, st); break;
+    }
+    HIP_TRY(hipGetLastError());
+    return MIXAQ_OK;
+}
+
+}  // namespace mixaq
+
+extern "C" int mixaq_scaled_quantize(const mixaq_rows* x, int32_t rows, int32_t columns, int32_t block_rows, const mixaq_rows* q,
+                                     void* stream)
+{
+    if (rows < 0 || columns < 1) return fail(MIXAQ_E_SHAPE, "need rows >= 0 and columns >= 1 (got %d, %d)", rows, columns);
+    if (block_rows != 1 && block_rows != SBLOCK) return fail(MIXAQ_E_SHAPE, "block_rows must be 1 or 128 (got %d)", block_rows);
+    if (rows == 0) return MIXAQ_OK;
+    const int32_t scale_rows = block_rows == 1 ? rows : blocks_of(rows);
+    int rc = check_rows(x, "x", columns, false, 0);
+    if (!rc) rc = check_rows(q, "q", columns, true, scale_rows);
+    if (rc) return rc;
+    if (q->type != MIXAQ_E4M3) return fail(MIXAQ_E_SHAPE, "q must be codes");
+    if (rows_overlap(*x, rows, columns, *q, rows, columns)) return fail(MIXAQ_E_SHAPE, "x and q overlap");
+    return launch_quantize(*x, rows, columns, block_rows, *q, (hipStream_t)stream);
+}
