@@ -147,8 +147,8 @@ def _ptr(t):
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:                                    # the current stream's handle, without a stream object around it (3 us)
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return C.c_void_p(stream.cuda_stream)
 
 
@@ -364,10 +364,10 @@ def _rows(t, name, scales=None, block_rows=1):
     (with block_rows 128: [.., blocks of rows])."""
     if t is None:
         return None
-    kind = ROW_TYPES.get(t.dtype)
-    if kind is None or t.dim() != 2:
+    kind, shape = ROW_TYPES.get(t.dtype), t.shape
+    if kind is None or len(shape) != 2:
         raise ValueError("%s must be a 2-D tensor of float32, float16, bfloat16 or float8_e4m3fn" % name)
-    rows, cols = t.shape
+    rows, cols = shape
     row, col = t.stride()
     if col != 1 and cols > 1:
         raise ValueError("%s: the values of a row must be adjacent (strides %d, %d)" % (name, row, col))
@@ -380,23 +380,26 @@ def _rows(t, name, scales=None, block_rows=1):
         return Rows(t.data_ptr(), row, kind, None, 0)
     if scales is None:
         raise ValueError("%s is float8_e4m3fn: its scales are missing" % name)
-    _vector(scales, name + "'s scales", (-(-cols // 128), -(-rows // block_rows)), strided=True)
-    return Rows(t.data_ptr(), row, kind, scales.data_ptr(), scales.stride(0) if scales.shape[0] > 1 else max(scales.shape[1], 1))
+    across = (rows + block_rows - 1) // block_rows
+    if scales.dtype is not torch.float32 or scales.shape != ((cols + 127) // 128, across) or (across > 1 and scales.stride(1) != 1):
+        raise ValueError("%s's scales must be float32 of shape (%d, %d) with adjacent columns (got %s, %s)"
+                         % (name, (cols + 127) // 128, across, scales.dtype, tuple(scales.shape)))
+    _on_device(scales, name)
+    return Rows(t.data_ptr(), row, kind, scales.data_ptr(), scales.stride(0) if cols > 128 else across)
 
 
 def _on_device(t, name):
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    at = t.get_device()
+    if at < 0 or at != torch._C._cuda_getDevice():
         raise ValueError("%s must be on the current device (it is on %s)" % (name, t.device))
 
 
-def _vector(t, name, shape, strided=False):
-    """Checks a float tensor of parameters or scales: contiguous, or with `strided` contiguous rows."""
+def _vector(t, name, shape):
+    """Checks a float tensor of parameters."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be float32 of shape %s (got %s, %s)" % (name, tuple(shape), t.dtype, tuple(t.shape)))
-    if not (t.is_contiguous() or (strided and (t.shape[1] <= 1 or t.stride(1) == 1))):
-        raise ValueError("%s must be contiguous" % name)
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be contiguous float32 of shape %s (got %s, %s)" % (name, shape, t.dtype, tuple(t.shape)))
     _on_device(t, name)
     return t
 
