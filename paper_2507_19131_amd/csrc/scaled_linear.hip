@@ -91,43 +91,45 @@ __device__ __forceinline__ void store16(T* p, int n, const float* v)
     store8(p + 8, n - 8, v + 8);
 }
 
-// The 32 outputs of one row that a lane holds, 16 from `col` on and 16 from col + 64 on.
-__device__ __forceinline__ void finish(const LinearArgs& A, float (&v)[32], int nb, int g, int row)
+// The outputs of one row that a lane holds: RUNS runs of 16 neighbouring ones, run i from `col` + offset(i) on; `LANES` lanes
+// (l, l + LANE_STEP, ..) hold a whole block of 128.
+template <int RUNS, int LANE_STEP, typename Offset>
+__device__ __forceinline__ void finish(const LinearArgs& A, float (&v)[16 * RUNS], int nb, int row, Offset offset)
 {
-    const int col = nb * SBLOCK + g * 16;
+    const int col = nb * SBLOCK;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int i = 0; i < RUNS; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            v[h * 16 + e] += A.bias[col + h * 64 + e];
-            if (A.gelu) v[h * 16 + e] = gelu(v[h * 16 + e]);
+            v[i * 16 + e] += A.bias[col + offset(i) + e];
+            if (A.gelu) v[i * 16 + e] = gelu(v[i * 16 + e]);
         }
     if (A.y_type == MIXAQ_E4M3) {
         unsigned m = 0;                                   // outputs beyond N are gelu(0) = 0 (or NaN where the whole row is)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) m = max(m, magnitude(v[e]));
-        m = max(m, (unsigned)__shfl_xor((int)m, 16, 64));
-        m = max(m, (unsigned)__shfl_xor((int)m, 32, 64));
+        for (int e = 0; e < 16 * RUNS; ++e) m = max(m, magnitude(v[e]));
+#pragma unroll
+        for (int d = LANE_STEP; d < 64; d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
         const BlockScale s = block_scale(m);
         if (row >= A.M) return;
-        if (g == 0) A.sy[nb * A.ldsy + row] = s.scale;
+        if ((threadIdx.x & 63) < LANE_STEP) A.sy[nb * A.ldsy + row] = s.scale;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int n = A.N - col - h * 64;
-            uint8_t* p = (uint8_t*)A.y + row * A.ldy + col + h * 64;
-            store_codes8(p, n, v + h * 16, s.inv);
-            store_codes8(p + 8, n - 8, v + h * 16 + 8, s.inv);
+        for (int i = 0; i < RUNS; ++i) {
+            const int n = A.N - col - offset(i);
+            uint8_t* p = (uint8_t*)A.y + row * A.ldy + col + offset(i);
+            store_codes8(p, n, v + i * 16, s.inv);
+            store_codes8(p + 8, n - 8, v + i * 16 + 8, s.inv);
         }
         return;
     }
     if (row >= A.M) return;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int n = A.N - col - h * 64;
-        const long long at = row * A.ldy + col + h * 64;
-        if (A.y_type == MIXAQ_F32) store16((float*)A.y + at, n, v + h * 16);
-        else if (A.y_type == MIXAQ_F16) store16((_Float16*)A.y + at, n, v + h * 16);
-        else store16((__bf16*)A.y + at, n, v + h * 16);
+    for (int i = 0; i < RUNS; ++i) {
+        const int n = A.N - col - offset(i);
+        const long long at = row * A.ldy + col + offset(i);
+        if (A.y_type == MIXAQ_F32) store16((float*)A.y + at, n, v + i * 16);
+        else if (A.y_type == MIXAQ_F16) store16((_Float16*)A.y + at, n, v + i * 16);
+        else store16((__bf16*)A.y + at, n, v + i * 16);
     }
 }
 
@@ -197,7 +199,173 @@ __global__ __launch_bounds__(256) void linear_kernel(LinearArgs A)
             for (int e = 0; e < 4; ++e) v[t * 4 + e] = fmaf(d[e], s, v[t * 4 + e]);
         }
     }
-    finish(A, v, nb, g, row);
+    finish<2, 16>(A, v, nb, row, [&](int i) { return i * 64 + g * 16; });
+}
+
+// ---- both operands through LDS ------------------------------------------------------------------------------------------
+// A workgroup of WM x WN waves computes 32 MT WM rows times 128 WN outputs, a wave 32 MT rows times one block of 128 outputs: the product of a
+// block's two scales is then a value per lane, and a row's codes need no exchange but between the two halves of a wave.  K goes in stages
+// of one block of 128 through two LDS buffers filled by direct loads; a stage travels under the products of the one before it.
+// Instructions of 32 x 32: the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, lane half h takes the 16-byte chunks
+// h, 2 + h, 4 + h and 6 + h of a row's 128 bytes.  Rows of x lie in LDS as 8 chunks whose places are turned by the row, so that the lanes that are
+// served together (eight rows, one chunk) meet all banks.
+// The direct loads are asm: as a builtin every LDS read behind them waits for all of them.
+__device__ __forceinline__ void request16(const void* uniform_src, unsigned lane_bytes, unsigned lds_dst)
+{
+    int m0;                                                              // given back: the compiler does not let an asm statement change it
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(lds_dst), "v"(lane_bytes), "s"(uniform_src) : "memory");
+}
+__device__ __forceinline__ void request4(const void* uniform_src, unsigned lane_bytes, unsigned lds_dst)
+{
+    int m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(lds_dst), "v"(lane_bytes), "s"(uniform_src) : "memory");
+}
+__device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)p; }
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+template <bool EXACT>
+__device__ __forceinline__ v16f product32(const v4i (&w)[4], const v4i (&x)[4])
+{
+    v16f d = {};
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][0], w[j][1]), widen(x[j][0], x[j][1]), d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][2], w[j][3]), widen(x[j][2], x[j][3]), d, 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            const v8i a = __builtin_shufflevector(w[j], w[j + 1], 0, 1, 2, 3, 4, 5, 6, 7), b = __builtin_shufflevector(x[j], x[j + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+            d = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, 0, 0, 0, 0, 0, 0);
+        }
+    }
+    return d;
+}
+
+constexpr int MOST_KB = 65536 / SBLOCK;
+constexpr int GROUP_M = 8;                        // row tiles that run beside one another
+
+template <bool EXACT, int MT, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int tiles_m, int tiles_n, FastDiv by_group)
+{
+    constexpr int W = WM * WN, TM = 32 * MT * WM;
+    constexpr int XP = TM * 8 / 64, WP = WN * 16, LPW = (XP + WP) / W;       // 1 KB pieces of a stage: of x, of w, and a wave's
+    static_assert((XP + WP) % W == 0 && TM / 64 <= W && LPW < 60, "whole pieces a wave");
+    __shared__ v4i xs[2][XP * 64], ws[2][WP * 64];
+    __shared__ float sxs[2][TM], sws[WN][MOST_KB];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
+    const int wm = wave / WN, wn = wave % WN;
+    // a run of tiles per XCD, in groups of GROUP_M row tiles with all their outputs, so that what its CUs read at one time meets in its L2
+    const int tiles = tiles_m * tiles_n, per_xcd = (tiles + 7) / 8;
+    const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per_xcd || t >= tiles) return;             // the whole workgroup
+    const int group = by_group(t), in = t - group * GROUP_M * tiles_n, gm = min(GROUP_M, tiles_m - group * GROUP_M);
+    const int tn = in / gm, tm = group * GROUP_M + in - tn * gm;
+    const int row0 = tm * TM, nb0 = tn * WN, nb = nb0 + wn;
+
+    const uint8_t* xb = A.x + (long long)row0 * A.ldx;
+    const float* sxb = A.sx + row0;
+    unsigned at[LPW];
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+        const int p = wave * LPW + i;                                        // this wave's i-th piece
+        const int r = p * 8 + (lane >> 3), chunk = (lane & 7) ^ (r & 7);
+        at[i] = p < XP ? (unsigned)(min(r, A.M - 1 - row0) * (int)A.ldx + chunk * 16) : lane * 16;
+    }
+    const unsigned srow = (unsigned)min(wave * 64 + lane, A.M - 1 - row0) * 4;
+    const unsigned lx = lds_address(xs), lw = lds_address(ws), ls = lds_address(sxs);
+    auto request = [&](int kb) {
+        const int b = kb & 1;
+        const bool tail = (kb + 1) * SBLOCK > A.K;                           // chunks behind a row's end: any of the row, the weights there are zero
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+            const int p = wave * LPW + i;
+            if (p < XP) {
+                unsigned o = at[i];
+                const int chunk = (lane & 7) ^ ((p * 8 + (lane >> 3)) & 7);
+                if (tail && kb * SBLOCK + chunk * 16 >= A.K) o -= chunk * 16;
+                request16(xb + kb * SBLOCK, o, lx + (b * XP + p) * 1024);
+            } else {
+                const int q = p - XP, n = min(nb0 + q / 16, A.NB - 1);
+                request16(A.w + ((long long)n * A.KB + kb) * (8 * TILE_BYTES) + (q % 16) * 1024, at[i], lw + (b * WP + q) * 1024);
+            }
+        }
+        if (wave < TM / 64) request4(sxb + kb * A.ldsx, srow, ls + (b * TM + wave * 64) * 4);
+    };
+    request(0);
+    for (int i = tid; i < WN * A.KB; i += W * 64) {
+        const int n = i / A.KB, kb = i - n * A.KB;
+        sws[n][kb] = A.sw[kb * A.NB + min(nb0 + n, A.NB - 1)];
+    }
+    v16f acc[MT][4] = {};
+    const int m0 = wm * 32 * MT;
+    for (int kb = 0; kb < A.KB; ++kb) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // this stage has landed, this wave's reads of the last one have returned
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (kb + 1 < A.KB) request(kb + 1);
+        const int b = kb & 1;
+        v4i x[MT][4];
+        float s[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int r = m0 + m * 32 + j;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[m][c] = xs[b][r * 8 + ((2 * c + h) ^ (r & 7))];
+            s[m] = sxs[b][r] * sws[wn][kb];
+        }
+        if ((A.K & 15) && kb == A.KB - 1) {                                  // what stands behind a row's end takes no part
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int left = A.K - kb * SBLOCK - (2 * c + h) * 16 - 4 * q;
+                    const int mask = left >= 4 ? -1 : left <= 0 ? 0 : (1 << (8 * left)) - 1;
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) x[m][c][q] &= mask;
+                }
+        }
+#pragma unroll
+        for (int T = 0; T < 4; ++T) {
+            v4i w[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w[c] = ws[b][wn * 1024 + ((2 * T + (j >> 4)) * 2 + (c >> 1)) * 64 + ((2 * c + h) & 3) * 16 + (j & 15)];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const v16f d = product32<EXACT>(w, x[m]);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[m][T][e] = fmaf(d[e], s[m], acc[m][T][e]);
+            }
+        }
+    }
+    if (nb >= A.NB) return;
+    // result e of the T-th instruction is its row 8 (e / 4) + 4 h + e % 4: of the outputs, with output_of, number 4 (2 (T % 2) + e / 8) + e % 4 of
+    // run 2 (e / 4 % 2) + h of 16, in half T / 2 of the block
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        float v[64];
+#pragma unroll
+        for (int T = 0; T < 4; ++T)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[((T >> 1) * 2 + (e >> 2 & 1)) * 16 + ((T & 1) * 2 + (e >> 3)) * 4 + (e & 3)] = acc[m][T][e];
+        finish<4, 32>(A, v, nb, row0 + m0 + m * 32 + j, [&](int i) { return (i >> 1) * 64 + (2 * (i & 1) + h) * 16; });
+    }
+}
+
+template <bool EXACT, int MT, int WM, int WN>
+int launch_tiles(const LinearArgs& A, hipStream_t st)
+{
+    constexpr int TM = 32 * MT * WM;
+    const int tiles_m = (int)(((long long)A.M + TM - 1) / TM), tiles_n = (A.NB + WN - 1) / WN;
+    const long long blocks = ((long long)tiles_m * tiles_n + 7) / 8 * 8;
+    if (blocks * WM * WN * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
+    hipLaunchKernelGGL((tile_kernel<EXACT, MT, WM, WN>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, tiles_m, tiles_n, FastDiv(GROUP_M * tiles_n));
+    HIP_TRY(hipGetLastError());
+    return MIXAQ_OK;
 }
 
 int round_up16(int v) { return (v + 15) / 16 * 16; }
@@ -319,7 +487,10 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
         rc = launch_quantize(*x, rows, K, 1, codes, st);
         if (rc) return rc;
     }
-    if (y->type == MIXAQ_F32 || y->type == MIXAQ_E4M3) hipLaunchKernelGGL(linear_kernel<true>, dim3(A.tiles), dim3(256), 0, st, A);
+    const bool exact = y->type == MIXAQ_F32 || y->type == MIXAQ_E4M3;
+    if ((long long)((rows + 255) / 256) * ((h->NB + 1) / 2) >= 256 && h->KB >= 4 && A.ldx < (1 << 22))
+        return exact ? launch_tiles<true, 1, 8, 1>(A, st) : launch_tiles<false, 2, 4, 2>(A, st);
+    if (exact) hipLaunchKernelGGL(linear_kernel<true>, dim3(A.tiles), dim3(256), 0, st, A);
     else hipLaunchKernelGGL(linear_kernel<false>, dim3(A.tiles), dim3(256), 0, st, A);
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
