@@ -27,28 +27,42 @@ struct NormArgs {
     const float *post_gamma, *post_beta, *pre_gamma, *pre_beta, *gate;
 };
 
-// Sum over the G lanes of a row; with more than a wave, through LDS (`part`: a float per wave, free again after the call).
+// Sum over the G lanes of a row; with more than a wave, through LDS (`part`: twice a float per wave, used in turn, so that one barrier is
+// enough: who writes a half again has passed the barrier of the other one, behind which nobody reads it any more).
 template <int G>
-__device__ __forceinline__ float row_sum(float v, float* part)
+__device__ __forceinline__ float row_sum(float v, float (*part)[4], int& turn)
 {
-#pragma unroll
-    for (int d = (G < 64 ? G : 64) / 2; d; d >>= 1) v += __shfl_xor(v, d, 64);
+    if constexpr (G == 16) return __uint_as_float(over16(__float_as_uint(v), SumOf()));
+    v = __uint_as_float(over64(__float_as_uint(v), SumOf()));
     if constexpr (G > 64) {
+        float* const p = part[turn];
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) p[threadIdx.x >> 6] = v;
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < G / 64; ++w) v += part[w];
+        v = (p[0] + p[1]) + (p[2] + p[3]);
     }
     return v;
 }
 
+// A vector of parameters: a lane's values of it.
+template <int V> struct Vector { float v[V][8]; };
+template <int G, int V, bool TINY>
+__device__ __forceinline__ void load_vector(Vector<V>& to, const float* from, const Eight (&c)[V], int C, float otherwise)
+{
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (from) load8<TINY>(from, c[j], C, to.v[j]);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to.v[j][e] = otherwise;
+    }
+}
+
 // One norm of a row whose values lie in registers, V times eight a lane: mean first, then the squares of what is left, so that
 // a large mean costs no digits.  Sums in binary32.
-template <int G, int V>
-__device__ __forceinline__ void norm_row(float (&v)[V][8], int kind, float eps, const float* gamma, const float* beta, const NormArgs& A,
-                                         int l, float* part)
+template <int G, int V, bool TINY>
+__device__ __forceinline__ void norm_row(float (&v)[V][8], int kind, float eps, const Vector<V>& gamma, const Vector<V>& beta, const Eight (&c)[V],
+                                         const NormArgs& A, float (*part)[4], int& turn)
 {
     float mean = 0.0f;
     if (kind == NORM_LAYER) {
@@ -56,101 +70,125 @@ __device__ __forceinline__ void norm_row(float (&v)[V][8], int kind, float eps, 
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += v[j][e];
-        mean = row_sum<G>(s, part) * A.inv_C;
+            for (int e = 0; e < 8; ++e) s += own8<TINY>(c[j], e, A.C) ? v[j][e] : 0.0f;
+        mean = row_sum<G>(s, part, turn) * A.inv_C;
     }
     float q = 0.0f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int n = A.C - (j * G + l) * 8;
+    for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[j][e] = e < n ? v[j][e] - mean : 0.0f;
-            q = fmaf(v[j][e], v[j][e], q);
+            v[j][e] -= mean;
+            const float o = own8<TINY>(c[j], e, A.C) ? v[j][e] : 0.0f;
+            q = fmaf(o, o, q);
         }
-    }
-    const float r = 1.0f / sqrtf(row_sum<G>(q, part) * A.inv_C + eps);
+    const float r = 1.0f / sqrtf(row_sum<G>(q, part, turn) * A.inv_C + eps);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int col = (j * G + l) * 8, n = A.C - col;
-        float g[8], b[8];
-        if (gamma) load8(gamma + col, n, g);
-        if (beta) load8(beta + col, n, b);
+    for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[j][e] *= r;
-            if (gamma) v[j][e] *= g[e];
-            if (beta) v[j][e] += b[e];
-        }
-    }
+        for (int e = 0; e < 8; ++e) v[j][e] = fmaf(v[j][e] * r, gamma.v[j][e], beta.v[j][e]);
 }
 
-template <int TX, int TB, int G, int V>
+// KEEP: the vectors of both norms stay in registers from row to row; else they come anew (from the caches) for every row, where V times eight
+// values of four of them would not fit beside the row.
+template <int TX, int TB, int G, int V, bool TINY>
 __global__ __launch_bounds__(256) void residual_norm_kernel(NormArgs A)
 {
     using X = typename TypeOf<TX>::T;
     using B = typename TypeOf<TB>::T;
-    __shared__ float part[4];
+    constexpr bool KEEP = V <= 2;
+    __shared__ float part[2][4];
+    int turn = 0;
     const int l = threadIdx.x % G, rows_at_once = 256 / G;
+    Eight c[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) c[j] = place8<TINY>((j * G + l) * 8, A.C);
+    Vector<V> post_gamma, post_beta, pre_gamma, pre_beta;
+    auto load_post = [&] {
+        load_vector<G, V, TINY>(post_gamma, A.post_gamma, c, A.C, 1.0f);
+        load_vector<G, V, TINY>(post_beta, A.post_beta, c, A.C, 0.0f);
+    };
+    auto load_pre = [&] {
+        load_vector<G, V, TINY>(pre_gamma, A.pre_gamma, c, A.C, 1.0f);
+        load_vector<G, V, TINY>(pre_beta, A.pre_beta, c, A.C, 0.0f);
+    };
+    if (KEEP && A.post) load_post();
+    if (KEEP && A.pre) load_pre();
     for (long long r0 = (long long)blockIdx.x * rows_at_once; r0 < A.rows; r0 += (long long)gridDim.x * rows_at_once) {
         const long long row = r0 + threadIdx.x / G;
-        const long long at = row < A.rows ? row : A.rows - 1;        // spare lanes take the last row along and store nothing
-        float y[V][8];
+        const bool real = row < A.rows;
+        const long long at = real ? row : A.rows - 1;                // spare lanes take the last row along and store nothing
+        float x[V][8], y[V][8], gate[V][8];
+#pragma unroll
+        for (int j = 0; j < V; ++j) load8<TINY>((const X*)A.x + at * A.ldx, c[j], A.C, x[j]);
         if (A.branch) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) load8((const B*)A.branch + at * A.ldb + (j * G + l) * 8, A.C - (j * G + l) * 8, y[j]);
-            if (A.post) norm_row<G, V>(y, A.post, A.post_eps, A.post_gamma, A.post_beta, A, l, part);
+            for (int j = 0; j < V; ++j) load8<TINY>((const B*)A.branch + at * A.ldb, c[j], A.C, y[j]);
+            if (A.gate) {
+                const float* from = A.gate + (long long)((int)at / A.rows_per_gate) * A.C;
+#pragma unroll
+                for (int j = 0; j < V; ++j) load8<TINY>(from, c[j], A.C, gate[j]);
+            }
+            if (A.post) {
+                if (!KEEP) load_post();
+                norm_row<G, V, TINY>(y, A.post, A.post_eps, post_gamma, post_beta, c, A, part, turn);
+            }
+            if (A.gate) {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[j][e] *= gate[j][e];
+            }
         }
-        const float* gate = A.gate ? A.gate + (long long)((int)at / A.rows_per_gate) * A.C : nullptr;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int col = (j * G + l) * 8, n = A.C - col;
-            float x[8], g[8];
-            load8((const X*)A.x + at * A.ldx + col, n, x);
-            if (gate) load8(gate + col, n, g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float b = A.branch ? (gate ? y[j][e] * g[e] : y[j][e]) : 0.0f;
-                y[j][e] = fmaf(A.residual_scale, x[e], b);
-            }
-            if (A.y && row < A.rows && n > 0) store8((X*)A.y + row * A.ldy + col, n, y[j]);
+            for (int e = 0; e < 8; ++e) y[j][e] = A.branch ? fmaf(A.residual_scale, x[j][e], y[j][e]) : A.residual_scale * x[j][e];
+            if (A.y && real) store8<TINY>((X*)A.y + row * A.ldy, c[j], A.C, y[j]);
         }
         if (!A.out) continue;
-        if (A.pre) norm_row<G, V>(y, A.pre, A.pre_eps, A.pre_gamma, A.pre_beta, A, l, part);
+        if (A.pre) {
+            if (!KEEP) load_pre();
+            norm_row<G, V, TINY>(y, A.pre, A.pre_eps, pre_gamma, pre_beta, c, A, part, turn);
+        }
+        if (A.out_type == MIXAQ_E4M3) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int col = (j * G + l) * 8, n = A.C - col;
-            if (A.out_type == MIXAQ_E4M3) {
-                const BlockScale s = block_scale(max16(max_magnitude(y[j])));
-                if (row < A.rows && n > 0) {
-                    store_codes8((uint8_t*)A.out + row * A.ldo + col, n, y[j], s.inv);
+            for (int j = 0; j < V; ++j) {
+                const BlockScale s = block_scale(max16(max_magnitude<TINY>(c[j], A.C, y[j])));
+                const int col = (j * G + l) * 8;
+                if (real && col < A.C) {
+                    store_codes8<TINY>((uint8_t*)A.out + row * A.ldo, c[j], A.C, y[j], s.inv);
                     if ((l & 15) == 0) A.scales[(long long)(col / SBLOCK) * A.lds + row] = s.scale;
                 }
-            } else if (row < A.rows && n > 0) {
-                if (A.out_type == MIXAQ_F32) store8((float*)A.out + row * A.ldo + col, n, y[j]);
-                else if (A.out_type == MIXAQ_F16) store8((_Float16*)A.out + row * A.ldo + col, n, y[j]);
-                else store8((__bf16*)A.out + row * A.ldo + col, n, y[j]);
+            }
+        } else if (real) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (A.out_type == MIXAQ_F32) store8<TINY>((float*)A.out + row * A.ldo, c[j], A.C, y[j]);
+                else if (A.out_type == MIXAQ_F16) store8<TINY>((_Float16*)A.out + row * A.ldo, c[j], A.C, y[j]);
+                else store8<TINY>((__bf16*)A.out + row * A.ldo, c[j], A.C, y[j]);
             }
         }
     }
 }
 
-template <int TX, int TB, int G, int V>
+template <int TX, int TB, int G, int V, bool TINY = false>
 void launch(const NormArgs& A, hipStream_t st)
 {
+    // as many workgroups as run at one time, each on every so many rows: the vectors are loaded once
     const long long groups = ((long long)A.rows + 256 / G - 1) / (256 / G);
-    hipLaunchKernelGGL((residual_norm_kernel<TX, TB, G, V>), dim3((unsigned)std::min(groups, 1LL << 23)), dim3(256), 0, st, A);
+    hipLaunchKernelGGL((residual_norm_kernel<TX, TB, G, V, TINY>), dim3((unsigned)std::min(groups, 2048LL)), dim3(256), 0, st, A);
 }
 // The lanes of a row: 16 as long as three vectors of eight hold their share, then a wave, then a workgroup.
 template <int TX, int TB>
 void launch_types(const NormArgs& A, hipStream_t st)
 {
-    if (A.C <= 128) launch<TX, TB, 16, 1>(A, st);
+    if (A.C < 8) launch<TX, TB, 16, 1, true>(A, st);
+    else if (A.C <= 128) launch<TX, TB, 16, 1>(A, st);
     else if (A.C <= 256) launch<TX, TB, 16, 2>(A, st);
-    else if (A.C <= 384) launch<TX, TB, 16, 3>(A, st);
     else if (A.C <= 512) launch<TX, TB, 64, 1>(A, st);
     else if (A.C <= 1024) launch<TX, TB, 64, 2>(A, st);
-    else if (A.C <= 2048) launch<TX, TB, 64, 4>(A, st);
+    else if (A.C <= 2048) launch<TX, TB, 256, 1>(A, st);
     else if (A.C <= 4096) launch<TX, TB, 256, 2>(A, st);
     else if (A.C <= 8192) launch<TX, TB, 256, 4>(A, st);
     else launch<TX, TB, 256, 8>(A, st);

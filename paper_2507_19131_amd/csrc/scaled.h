@@ -22,46 +22,67 @@ template <int TYPE> struct TypeOf;
 template <> struct TypeOf<MIXAQ_F32> { using T = float; };
 template <> struct TypeOf<MIXAQ_F16> { using T = _Float16; };
 template <> struct TypeOf<MIXAQ_BF16> { using T = __bf16; };
+template <> struct TypeOf<MIXAQ_E4M3> { using T = uint8_t; };
 
-// n of the eight values from p on (all of them: n >= 8), zero for the others.  Global memory takes vector accesses at any address, so
-// rows of odd stride need no form of their own; only the values that lie behind the row's end are taken one by one.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, float v[8])
+// A lane's eight columns.  The last lane of a row of C columns takes its last eight, and of those only the ones from `first` on are its
+// own; lanes behind the row take the same and own none.  So every load is whole and in the row, without a branch between it and the next one, and
+// rows of any stride and length take the same path: global memory takes vector accesses at any address.  (Of fewer than eight columns lane 0 owns
+// all, one by one: TINY.)
+struct Eight { int at, first; };
+template <bool TINY>
+__device__ __forceinline__ Eight place8(int col, int C)
+{
+    if (TINY) return {0, col == 0 ? 0 : 8};
+    const int at = min(col, C - 8);
+    return {at, min(col - at, 8)};
+}
+template <bool TINY, typename T>
+__device__ __forceinline__ void load8(const T* row, Eight c, int C, float v[8])
 {
     T t[8];
-    if (n >= 8) {
-        __builtin_memcpy(t, p, sizeof(t));
+    if constexpr (TINY) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
+        for (int e = 0; e < 8; ++e) t[e] = e < C ? row[e] : (T)0.0f;
     } else {
+        __builtin_memcpy(t, row + c.at, sizeof(t));
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)p[e] : 0.0f;
+    for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
+}
+// whether element e of a lane's eight is its own
+template <bool TINY>
+__device__ __forceinline__ bool own8(Eight c, int e, int C) { return e >= c.first && (!TINY || e < C); }
+
+template <bool TINY, typename T>
+__device__ __forceinline__ void put8(T* row, Eight c, int C, const T t[8])
+{
+    if (!TINY && c.first == 0) {
+        __builtin_memcpy(row + c.at, t, 8 * sizeof(T));
+    } else if (c.first < 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (own8<TINY>(c, e, C)) row[c.at + e] = t[e];
     }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int n, const float v[8])
+template <bool TINY, typename T>
+__device__ __forceinline__ void store8(T* row, Eight c, int C, const float v[8])
 {
     T t[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) t[e] = (T)v[e];
-    if (n >= 8) {
-        __builtin_memcpy(p, t, sizeof(t));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = t[e];
-    }
+    put8<TINY>(row, c, C, t);
 }
 
 // ---- the scale of a block -------------------------------------------------------------------------------------
 // Magnitudes are compared as bit patterns, which order like the numbers with infinity and then NaN on top: a block that holds one
 // cannot hide it.
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-__device__ __forceinline__ unsigned max_magnitude(const float v[8])
+template <bool TINY>
+__device__ __forceinline__ unsigned max_magnitude(Eight c, int C, const float v[8])
 {
     unsigned m = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, magnitude(v[e]));
+    for (int e = 0; e < 8; ++e) m = max(m, own8<TINY>(c, e, C) ? magnitude(v[e]) : 0u);
     return m;
 }
 struct BlockScale { float scale, inv; };           // both NaN for a block that holds a NaN or an infinity
@@ -81,24 +102,37 @@ __device__ __forceinline__ int codes4(float a, float b, float c, float d, float 
     w = __builtin_amdgcn_cvt_pk_fp8_f32(q(c), q(d), w, true);
     return inv == inv ? w : 0x7f7f7f7f;
 }
-__device__ __forceinline__ void store_codes8(uint8_t* p, int n, const float v[8], float inv)
+template <bool TINY>
+__device__ __forceinline__ void store_codes8(uint8_t* row, Eight c, int C, const float v[8], float inv)
 {
     const int w[2] = {codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv)};
-    if (n >= 8) {
-        __builtin_memcpy(p, w, 8);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
-    }
+    uint8_t t[8];
+    __builtin_memcpy(t, w, 8);
+    put8<TINY>(row, c, C, t);
 }
-// over the 16 lanes that hold a block of 128 columns, eight each
-__device__ __forceinline__ unsigned max16(unsigned m)
+
+// ---- exchanges between lanes, all in the vector unit ------------------------------------------------------------
+template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+template <typename Op>
+__device__ __forceinline__ unsigned over16(unsigned v, Op op)         // of 16 lanes
 {
-#pragma unroll
-    for (int d = 8; d; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
-    return m;
+    v = op(v, dpp<0xB1>(v));                                          // neighbours
+    v = op(v, dpp<0x4E>(v));                                          // pairs
+    v = op(v, dpp<0x141>(v));                                         // quads, by the mirror of eight lanes
+    return op(v, dpp<0x140>(v));                                      // eights, by the mirror of 16
 }
+template <typename Op>
+__device__ __forceinline__ unsigned over64(unsigned v, Op op)
+{
+    v = over16(v, op);
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = op(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return op(b[0], b[1]);
+}
+struct MaxOf { __device__ unsigned operator()(unsigned a, unsigned b) const { return max(a, b); } };
+struct SumOf { __device__ unsigned operator()(unsigned a, unsigned b) const { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); } };
+__device__ __forceinline__ unsigned max16(unsigned m) { return over16(m, MaxOf()); }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
 constexpr long long MOST_THREADS = 1LL << 32;      // of one launch

@@ -62,25 +62,22 @@ struct QuantArgs {
 
 // One block of a row is 16 lanes with eight values each; a wave takes 16 rows of one block of columns, four at a time, and the waves
 // beside it the next blocks of the same rows.
-template <typename T>
+template <typename T, bool TINY>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs A)
 {
     const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
     for (int u = blockIdx.x * 4 + (threadIdx.x >> 6); u < A.units; u += gridDim.x * 4) {
         const int rg = A.by_nb(u), b = u - rg * A.nb;
-        const int col = b * SBLOCK + l * 8, n = A.cols - col;
+        const Eight c = place8<TINY>(b * SBLOCK + l * 8, A.cols);
         float v[4][8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = rg * 16 + j * 4 + g;
-            load8((const T*)A.x + (long long)min(row, A.rows - 1) * A.ldx + col, n, v[j]);
-        }
+        for (int j = 0; j < 4; ++j) load8<TINY>((const T*)A.x + (long long)min(rg * 16 + j * 4 + g, A.rows - 1) * A.ldx, c, A.cols, v[j]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int row = rg * 16 + j * 4 + g;
-            const BlockScale s = block_scale(max16(max_magnitude(v[j])));
+            const BlockScale s = block_scale(max16(max_magnitude<TINY>(c, A.cols, v[j])));
             if (row < A.rows) {
-                if (n > 0) store_codes8(A.codes + (long long)row * A.ldc + col, n, v[j], s.inv);
+                store_codes8<TINY>(A.codes + (long long)row * A.ldc, c, A.cols, v[j], s.inv);
                 if (l == 0) A.scales[b * A.lds + row] = s.scale;
             }
         }
@@ -88,22 +85,20 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs A)
 }
 
 // A workgroup per 128 x 128 tile, held in registers between its maximum and its codes.
-template <typename T>
+template <typename T, bool TINY>
 __global__ __launch_bounds__(256) void quantize_tiles_kernel(QuantArgs A)
 {
     __shared__ unsigned part[4];
     const int tr = A.by_nb(blockIdx.x), b = blockIdx.x - tr * A.nb;
-    const int l = threadIdx.x & 15, g = threadIdx.x >> 4, col = b * SBLOCK + l * 8, n = A.cols - col;
+    const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const Eight c = place8<TINY>(b * SBLOCK + l * 8, A.cols);
     float v[8][8];
     unsigned m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int row = tr * SBLOCK + j * 16 + g;
-        load8((const T*)A.x + (long long)min(row, A.rows - 1) * A.ldx + col, n, v[j]);
-        if (row < A.rows) m = max(m, max_magnitude(v[j]));
-    }
+    for (int j = 0; j < 8; ++j) load8<TINY>((const T*)A.x + (long long)min(tr * SBLOCK + j * 16 + g, A.rows - 1) * A.ldx, c, A.cols, v[j]);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
+    for (int j = 0; j < 8; ++j) m = max(m, max_magnitude<TINY>(c, A.cols, v[j]));        // (the last row once more is no other maximum)
+    m = over64(m, MaxOf());
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
     __syncthreads();
     const BlockScale s = block_scale(max(max(part[0], part[1]), max(part[2], part[3])));
@@ -111,16 +106,22 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(QuantArgs A)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int row = tr * SBLOCK + j * 16 + g;
-        if (row < A.rows && n > 0) store_codes8(A.codes + (long long)row * A.ldc + col, n, v[j], s.inv);
+        if (row < A.rows) store_codes8<TINY>(A.codes + (long long)row * A.ldc, c, A.cols, v[j], s.inv);
     }
 }
 
-template <int TYPE>
+template <typename T, bool TINY>
 void launch(const QuantArgs& A, int block_rows, hipStream_t st)
 {
+    if (block_rows == 1) hipLaunchKernelGGL((quantize_rows_kernel<T, TINY>), dim3(std::min((A.units + 3) / 4, 1 << 22)), dim3(256), 0, st, A);
+    else hipLaunchKernelGGL((quantize_tiles_kernel<T, TINY>), dim3(A.units), dim3(256), 0, st, A);
+}
+template <int TYPE>
+void launch_type(const QuantArgs& A, int block_rows, hipStream_t st)
+{
     using T = typename TypeOf<TYPE>::T;
-    if (block_rows == 1) hipLaunchKernelGGL(quantize_rows_kernel<T>, dim3(std::min((A.units + 3) / 4, 1 << 22)), dim3(256), 0, st, A);
-    else hipLaunchKernelGGL(quantize_tiles_kernel<T>, dim3(A.units), dim3(256), 0, st, A);
+    if (A.cols < 8) launch<T, true>(A, block_rows, st);
+    else launch<T, false>(A, block_rows, st);
 }
 
 }  // namespace
@@ -141,9 +142,9 @@ int launch_quantize(const mixaq_rows& x, int32_t rows, int32_t columns, int32_t 
     A.units = (int)units;
     A.by_nb = FastDiv(A.nb);
     switch (x.type) {
-    case MIXAQ_F32: launch<MIXAQ_F32>(A, block_rows, st); break;
-    case MIXAQ_F16: launch<MIXAQ_F16>(A, block_rows, st); break;
-    default: launch<MIXAQ_BF16>(A, block_rows, st); break;
+    case MIXAQ_F32: launch_type<MIXAQ_F32>(A, block_rows, st); break;
+    case MIXAQ_F16: launch_type<MIXAQ_F16>(A, block_rows, st); break;
+    default: launch_type<MIXAQ_BF16>(A, block_rows, st); break;
     }
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
