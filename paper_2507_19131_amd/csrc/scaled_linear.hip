@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "arena.h"
 
@@ -84,52 +85,67 @@ __device__ __forceinline__ float gelu(float v)
     return (v < 0.0f ? 0.0f : v) - 0.5f * a * (p * t * e);
 }
 
-template <typename T>
-__device__ __forceinline__ void store16(T* p, int n, const float* v)
-{
-    store8(p, n, v);
-    store8(p + 8, n - 8, v + 8);
-}
-
-// The outputs of one row that a lane holds: RUNS runs of 16 neighbouring ones, run i from `col` + offset(i) on; `LANES` lanes
-// (l, l + LANE_STEP, ..) hold a whole block of 128.
-template <int RUNS, int LANE_STEP, typename Offset>
+// The outputs of one row that a lane holds: RUNS runs of 16 neighbouring ones, run i from column offset(i) of block nb on; the lanes
+// l, l + LANE_STEP, .. hold the whole block.  A block inside the matrix takes the short way, the last one stores value by value.
+template <int YT, int RUNS, int LANE_STEP, typename Offset>
 __device__ __forceinline__ void finish(const LinearArgs& A, float (&v)[16 * RUNS], int nb, int row, Offset offset)
 {
+    using T = typename TypeOf<YT>::T;
     const int col = nb * SBLOCK;
+    T* const y = (T*)A.y + (long long)min(row, A.M - 1) * A.ldy + col;
+    auto activate = [&](int i) {
+        float b[16];
+        __builtin_memcpy(b, A.bias + col + offset(i), sizeof(b));
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i)
+        for (int e = 0; e < 16; ++e) v[i * 16 + e] += b[e];
+        if (A.gelu) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            v[i * 16 + e] += A.bias[col + offset(i) + e];
-            if (A.gelu) v[i * 16 + e] = gelu(v[i * 16 + e]);
+            for (int e = 0; e < 16; ++e) v[i * 16 + e] = gelu(v[i * 16 + e]);
         }
-    if (A.y_type == MIXAQ_E4M3) {
-        unsigned m = 0;                                   // outputs beyond N are gelu(0) = 0 (or NaN where the whole row is)
-#pragma unroll
-        for (int e = 0; e < 16 * RUNS; ++e) m = max(m, magnitude(v[e]));
-#pragma unroll
-        for (int d = LANE_STEP; d < 64; d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
-        const BlockScale s = block_scale(m);
+    };
+    auto store = [&](int i, const T (&t)[16]) {
         if (row >= A.M) return;
-        if ((threadIdx.x & 63) < LANE_STEP) A.sy[nb * A.ldsy + row] = s.scale;
+        if (col + SBLOCK <= A.N) {
+            __builtin_memcpy(y + offset(i), t, sizeof(t));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (col + offset(i) + e < A.N) y[offset(i) + e] = t[e];
+        }
+    };
+    if constexpr (YT == MIXAQ_E4M3) {
+        unsigned largest = 0;                             // outputs beyond N are gelu(0) = 0 (or NaN where the whole row is)
 #pragma unroll
         for (int i = 0; i < RUNS; ++i) {
-            const int n = A.N - col - offset(i);
-            uint8_t* p = (uint8_t*)A.y + row * A.ldy + col + offset(i);
-            store_codes8(p, n, v + i * 16, s.inv);
-            store_codes8(p + 8, n - 8, v + i * 16 + 8, s.inv);
+            activate(i);
+            asm volatile("" ::: "memory");                // one run's bias at a time
         }
-        return;
-    }
-    if (row >= A.M) return;
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i) {
-        const int n = A.N - col - offset(i);
-        const long long at = row * A.ldy + col + offset(i);
-        if (A.y_type == MIXAQ_F32) store16((float*)A.y + at, n, v + i * 16);
-        else if (A.y_type == MIXAQ_F16) store16((_Float16*)A.y + at, n, v + i * 16);
-        else store16((__bf16*)A.y + at, n, v + i * 16);
+        for (int e = 0; e < 16 * RUNS; ++e) largest = max(largest, magnitude(v[e]));
+#pragma unroll
+        for (int d = LANE_STEP; d < 64; d <<= 1) largest = max(largest, (unsigned)__shfl_xor((int)largest, d, 64));
+        const BlockScale s = block_scale(largest);
+        if (row < A.M && (threadIdx.x & 63) < LANE_STEP) A.sy[nb * A.ldsy + row] = s.scale;
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i) {
+            T t[16];
+#pragma unroll
+            for (int q = 0; q < 16; q += 4) {
+                const int w = codes4(v[i * 16 + q], v[i * 16 + q + 1], v[i * 16 + q + 2], v[i * 16 + q + 3], s.inv);
+                __builtin_memcpy(t + q, &w, 4);
+            }
+            store(i, t);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i) {
+            activate(i);
+            T t[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) t[e] = (T)v[i * 16 + e];
+            store(i, t);
+            asm volatile("" ::: "memory");
+        }
     }
 }
 
@@ -155,6 +171,8 @@ __device__ __forceinline__ v4i load_codes(const uint8_t* row, int k, int K)
 // 1.5e-5 of the results' root mean square on normal values, 2.8e-5 with an outlier channel.  That is a hundredth of what rounding to bf16
 // costs and a tenth of f16's, but not binary32: results of 32 bits, and those that become codes, whose scale is kept in 32 bits, are summed
 // by the f16 instruction (e4m3 values are f16 values, their products exact, 1e-8), which takes twice the time.
+constexpr bool exact_sums(int y_type) { return y_type == MIXAQ_F32 || y_type == MIXAQ_E4M3; }
+
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
@@ -180,7 +198,7 @@ __device__ __forceinline__ v4f product(v4i w0, v4i w1, v4i x0, v4i x1)
 }
 
 // A wave per 16 rows and 128 outputs, operands straight from memory.
-template <bool EXACT>
+template <int YT>
 __global__ __launch_bounds__(256) void linear_kernel(LinearArgs A)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4;
@@ -194,21 +212,20 @@ __global__ __launch_bounds__(256) void linear_kernel(LinearArgs A)
         const v4i* w = (const v4i*)(A.w + ((long long)nb * A.KB + kb) * 8 * TILE_BYTES) + lane;
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            const v4f d = product<EXACT>(w[t * 128], w[t * 128 + 64], x0, x1);
+            const v4f d = product<exact_sums(YT)>(w[t * 128], w[t * 128 + 64], x0, x1);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[t * 4 + e] = fmaf(d[e], s, v[t * 4 + e]);
         }
     }
-    finish<2, 16>(A, v, nb, row, [&](int i) { return i * 64 + g * 16; });
+    finish<YT, 2, 16>(A, v, nb, row, [&](int i) { return i * 64 + g * 16; });
 }
 
 // ---- both operands through LDS ------------------------------------------------------------------------------------------
 // A workgroup of WM x WN waves computes 32 MT WM rows times 128 WN outputs, a wave 32 MT rows times one block of 128 outputs: the product of a
 // block's two scales is then a value per lane, and a row's codes need no exchange but between the two halves of a wave.  K goes in stages
 // of one block of 128 through two LDS buffers filled by direct loads; a stage travels under the products of the one before it.
-// Instructions of 32 x 32: the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, lane half h takes the 16-byte chunks
-// h, 2 + h, 4 + h and 6 + h of a row's 128 bytes.  Rows of x lie in LDS as 8 chunks whose places are turned by the row, so that the lanes that are
-// served together (eight rows, one chunk) meet all banks.
+// Rows of x lie in LDS as 8 chunks of 16 bytes whose places are turned by half the row's number, so that the 16 lanes that are served
+// together (16 rows, one chunk) meet all 64 banks.
 // The direct loads are asm: as a builtin every LDS read behind them waits for all of them.
 __device__ __forceinline__ void request16(const void* uniform_src, unsigned lane_bytes, unsigned lds_dst)
 {
@@ -226,35 +243,34 @@ __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigne
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-template <bool EXACT>
-__device__ __forceinline__ v16f product32(const v4i (&w)[4], const v4i (&x)[4])
+// one half of a product of a block: the chunks 2 HALF and 2 HALF + 1 of a lane
+template <bool EXACT, int HALF>
+__device__ __forceinline__ v16f half_product(const v4i (&w)[4], const v4i (&x)[4], v16f d)
 {
-    v16f d = {};
     if constexpr (EXACT) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 2 * HALF; j < 2 * HALF + 2; ++j) {
             d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][0], w[j][1]), widen(x[j][0], x[j][1]), d, 0, 0, 0);
             d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][2], w[j][3]), widen(x[j][2], x[j][3]), d, 0, 0, 0);
         }
+        return d;
     } else {
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-            const v8i a = __builtin_shufflevector(w[j], w[j + 1], 0, 1, 2, 3, 4, 5, 6, 7), b = __builtin_shufflevector(x[j], x[j + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-            d = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, 0, 0, 0, 0, 0, 0);
-        }
+        const v8i a = __builtin_shufflevector(w[2 * HALF], w[2 * HALF + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+        const v8i b = __builtin_shufflevector(x[2 * HALF], x[2 * HALF + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, 0, 0, 0, 0, 0, 0);
     }
-    return d;
 }
 
 constexpr int MOST_KB = 65536 / SBLOCK;
 constexpr int GROUP_M = 8;                        // row tiles that run beside one another
 
-template <bool EXACT, int MT, int WM, int WN>
+template <int YT, int MT, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int tiles_m, int tiles_n, FastDiv by_group)
 {
+    constexpr bool EXACT = exact_sums(YT);
     constexpr int W = WM * WN, TM = 32 * MT * WM;
-    constexpr int XP = TM * 8 / 64, WP = WN * 16, LPW = (XP + WP) / W;       // 1 KB pieces of a stage: of x, of w, and a wave's
-    static_assert((XP + WP) % W == 0 && TM / 64 <= W && LPW < 60, "whole pieces a wave");
+    constexpr int XP = TM * 8 / 64, WP = WN * 16, XL = XP / W, WL = WP / W;  // 1 KB pieces of a stage, of x and of w, and a wave's
+    static_assert(XP % W == 0 && WP % W == 0 && TM / 64 <= W, "whole pieces a wave");
     __shared__ v4i xs[2][XP * 64], ws[2][WP * 64];
     __shared__ float sxs[2][TM], sws[WN][MOST_KB];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
@@ -265,105 +281,250 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
     if ((int)(blockIdx.x >> 3) >= per_xcd || t >= tiles) return;             // the whole workgroup
     const int group = by_group(t), in = t - group * GROUP_M * tiles_n, gm = min(GROUP_M, tiles_m - group * GROUP_M);
     const int tn = in / gm, tm = group * GROUP_M + in - tn * gm;
-    const int row0 = tm * TM, nb0 = tn * WN, nb = nb0 + wn;
+    const int row0 = tm * TM, nb0 = tn * WN, nb = nb0 + wn, KB = A.KB;
 
+    // what this wave requests: rows (wave XL + i) 8 + lane / 8 of x, whose lanes take the chunk that belongs in their place, and pieces
+    // wave WL + i of w; the first waves the scales of 64 rows each
     const uint8_t* xb = A.x + (long long)row0 * A.ldx;
     const float* sxb = A.sx + row0;
-    unsigned at[LPW];
+    static_assert(XL % 2 == 0, "the parity of a piece is that of i");
+    const int chunk[2] = {((lane & 7) ^ (lane >> 4)) * 16, ((lane & 7) ^ (lane >> 4) ^ 4) * 16};     // of even and of odd pieces
+    unsigned at[XL];
 #pragma unroll
-    for (int i = 0; i < LPW; ++i) {
-        const int p = wave * LPW + i;                                        // this wave's i-th piece
-        const int r = p * 8 + (lane >> 3), chunk = (lane & 7) ^ (r & 7);
-        at[i] = p < XP ? (unsigned)(min(r, A.M - 1 - row0) * (int)A.ldx + chunk * 16) : lane * 16;
-    }
-    const unsigned srow = (unsigned)min(wave * 64 + lane, A.M - 1 - row0) * 4;
+    for (int i = 0; i < XL; ++i) at[i] = (unsigned)(min((wave * XL + i) * 8 + (lane >> 3), A.M - 1 - row0) * (int)A.ldx + chunk[i & 1]);
+    const uint8_t* wb = A.w + (long long)min(nb0 + wave * WL / 16, A.NB - 1) * KB * (8 * TILE_BYTES) + wave * WL % 16 * 1024;
+    const int swave = wave % (TM / 64);                                      // (where there are more waves, twice)
+    const unsigned srow = (unsigned)min(swave * 64 + lane, A.M - 1 - row0) * 4;
     const unsigned lx = lds_address(xs), lw = lds_address(ws), ls = lds_address(sxs);
-    auto request = [&](int kb) {
-        const int b = kb & 1;
-        const bool tail = (kb + 1) * SBLOCK > A.K;                           // chunks behind a row's end: any of the row, the weights there are zero
-#pragma unroll
-        for (int i = 0; i < LPW; ++i) {
-            const int p = wave * LPW + i;
-            if (p < XP) {
-                unsigned o = at[i];
-                const int chunk = (lane & 7) ^ ((p * 8 + (lane >> 3)) & 7);
-                if (tail && kb * SBLOCK + chunk * 16 >= A.K) o -= chunk * 16;
-                request16(xb + kb * SBLOCK, o, lx + (b * XP + p) * 1024);
-            } else {
-                const int q = p - XP, n = min(nb0 + q / 16, A.NB - 1);
-                request16(A.w + ((long long)n * A.KB + kb) * (8 * TILE_BYTES) + (q % 16) * 1024, at[i], lw + (b * WP + q) * 1024);
-            }
-        }
-        if (wave < TM / 64) request4(sxb + kb * A.ldsx, srow, ls + (b * TM + wave * 64) * 4);
+    const int kb_tail = A.K % SBLOCK ? KB - 1 : KB;                          // chunks behind a row's end: the row's first, the weights there are zero
+    auto request_x = [&](int kb, int i) {
+        unsigned o = at[i];
+        if (kb >= kb_tail && kb * SBLOCK + chunk[i & 1] >= A.K) o -= chunk[i & 1];
+        request16(xb + kb * SBLOCK, o, lx + ((kb & 1) * XP + wave * XL + i) * 1024);
     };
-    request(0);
-    for (int i = tid; i < WN * A.KB; i += W * 64) {
-        const int n = i / A.KB, kb = i - n * A.KB;
-        sws[n][kb] = A.sw[kb * A.NB + min(nb0 + n, A.NB - 1)];
-    }
-    v16f acc[MT][4] = {};
-    const int m0 = wm * 32 * MT;
-    for (int kb = 0; kb < A.KB; ++kb) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // this stage has landed, this wave's reads of the last one have returned
+    auto request_w = [&](int kb, int i) { request16(wb + (long long)kb * (8 * TILE_BYTES) + i * 1024, lane * 16, lw + ((kb & 1) * WP + wave * WL + i) * 1024); };
+    auto request_s = [&](int kb) { request4(sxb + kb * A.ldsx, srow, ls + ((kb & 1) * TM + swave * 64) * 4); };
+    auto landed = [&] {                                                      // every wave's requests, and its reads of the other buffer have returned
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (kb + 1 < A.KB) request(kb + 1);
-        const int b = kb & 1;
-        v4i x[MT][4];
-        float s[MT];
+    };
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+    for (int i = 0; i < XL; ++i) request_x(0, i);
+#pragma unroll
+    for (int i = 0; i < WL; ++i) request_w(0, i);
+    request_s(0);
+    for (int i = tid; i < WN * KB; i += W * 64) {
+        const int n = i / KB, kb = i - n * KB;
+        sws[n][kb] = A.sw[kb * A.NB + min(nb0 + n, A.NB - 1)];
+    }
+    const int m0 = wm * 32 * MT;
+    auto scale_of = [&](int kb, int row) { return sxs[kb & 1][row] * sws[wn][kb]; };
+    // `left`: of the row's bytes from a chunk on; what stands behind them takes no part
+    auto cut = [&](v4i& c, int left) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c[q] &= left >= 4 * q + 4 ? -1 : left <= 4 * q ? 0 : (1 << (8 * (left - 4 * q))) - 1;
+    };
+    auto all_stages = [&](auto&& stage, auto&& cut_rows) {
+        constexpr std::true_type yes;
+        constexpr std::false_type no;
+        int kb = 0;
+#pragma unroll 1
+        for (; kb < KB - 2; ++kb) stage(kb, yes, yes);
+        if (KB > 1) stage(kb++, yes, no);
+        if (A.K & 15) cut_rows(A.K - kb * SBLOCK);
+        stage(kb, no, no);
+    };
+    landed();
+    if (KB > 1) {
+#pragma unroll
+        for (int i = 0; i < XL; ++i) request_x(1, i);
+#pragma unroll
+        for (int i = 0; i < WL; ++i) request_w(1, i);
+        request_s(1);
+    }
+    // The stages.  Beside a product run the sums of an earlier one, whose result is there by then: matrix and vector work of a wave side by side.  What
+    // a product needs of LDS is read some products ahead; behind the last read of a stage the waves meet, and its buffer is requested anew.
+    // (Without branches in a stage: the compiler moves the sums behind any, away from the matrix instructions.)
+    if constexpr (!EXACT) {
+        // instructions of 16 x 16 x 128, one a block: tile T of the packed eight, rows 16 i .. of the wave's; lane group g takes chunks g and 4 + g
+        constexpr int MI = 2 * MT, P = 8 * MI, BEHIND = 2;
+        static_assert(MI >= BEHIND, "the products of a stage that are added in the next one");
+        const int c = lane & 15, g = lane >> 4;
+        v4f acc[MI][8] = {}, d[4] = {};
+        v4i x[MI][2], w[3][2];
+        float s[MI], s_last[BEHIND] = {};
+        const v4i* const xr[2] = {&xs[0][(m0 + c) * 8 + (g ^ (c >> 1))], &xs[0][(m0 + c) * 8 + ((g + 4) ^ (c >> 1))]};
+        const v4i* const wr = &ws[0][wn * 1024 + lane];
+        auto read_x = [&](int kb, int i) {
+            x[i][0] = xr[0][(kb & 1) * (XP * 64) + i * 128];
+            x[i][1] = xr[1][(kb & 1) * (XP * 64) + i * 128];
+        };
+        auto read_w = [&](int kb, int T, int to) {
+            w[to][0] = wr[(kb & 1) * (WP * 64) + T * 128];
+            w[to][1] = wr[(kb & 1) * (WP * 64) + T * 128 + 64];
+        };
+        auto add = [&](int p, float scale) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[p % MI][p / MI][e] = fmaf(d[p & 3][e], scale, acc[p % MI][p / MI][e]);
+        };
+        read_w(0, 0, 0);
+        read_w(0, 1, 1);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            read_x(0, i);
+            s[i] = scale_of(0, m0 + i * 16 + c);
+        }
+        all_stages([&](int kb, auto more, auto request) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int T = p / MI, i = p % MI, behind = (p + P - BEHIND) % P;
+                if (i == 0 && T < 6) read_w(kb, T + 2, (T + 2) % 3);
+                if (i == 0 && T == 6 && more) landed();
+                if (i == 0 && T >= 6 && more) read_w(kb + 1, T - 6, (T + 2) % 3);
+                __builtin_amdgcn_sched_barrier(0);
+                d[p & 3] = product<false>(w[T % 3][0], w[T % 3][1], x[i][0], x[i][1]);
+                __builtin_amdgcn_sched_barrier(0);
+                add(behind, p < BEHIND ? s_last[p] : s[behind % MI]);
+                if (T == 7 && more) read_x(kb + 1, i);
+                if (T >= 6 && request) {                                     // a request a product
+                    const int q = p - 6 * MI, per = (XL + WL + 2 * MI - 1) / (2 * MI);
+#pragma unroll
+                    for (int k = q * per; k < (q + 1) * per; ++k) {
+                        if (k < XL) request_x(kb + 2, k);
+                        else if (k < XL + WL) request_w(kb + 2, k - XL);
+                    }
+                    if (q == 2 * MI - 1) request_s(kb + 2);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (more) {
+                // w of the next stage's first tiles lie where (8 + T) % 3 says: back to their places
+                const v4i a0 = w[2][0], a1 = w[2][1], b0 = w[0][0], b1 = w[0][1];
+                w[0][0] = a0; w[0][1] = a1; w[1][0] = b0; w[1][1] = b1;
+#pragma unroll
+                for (int b = 0; b < BEHIND; ++b) s_last[b] = s[MI - BEHIND + b];
+#pragma unroll
+                for (int i = 0; i < MI; ++i) s[i] = scale_of(kb + 1, m0 + i * 16 + c);
+            }
+        }, [&](int left) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                cut(x[i][0], left - g * 16);
+                cut(x[i][1], left - g * 16 - 64);
+            }
+        });
+#pragma unroll
+        for (int b = 0; b < BEHIND; ++b) add(P - BEHIND + b, s[MI - BEHIND + b]);
+        if (nb >= A.NB) return;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            float v[32];
+#pragma unroll
+            for (int T = 0; T < 8; ++T)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[T * 4 + e] = acc[i][T][e];
+            finish<YT, 2, 16>(A, v, nb, row0 + m0 + i * 16 + c, [&](int r) { return r * 64 + g * 16; });
+        }
+    } else {
+        // instructions of 32 x 32 x 16 (those of 16 x 16 have half their rate): the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, lane
+        // half h takes the chunks h, 2 + h, 4 + h and 6 + h of a row
+        constexpr int P = 4 * MT;
+        v16f acc[MT][4] = {}, d[2] = {};
+        v4i x[MT][4], w[2][4];
+        float s[MT], s_last = 0.0f;                                          // of this stage's rows; of the product still to be added
+        auto read_x = [&](int kb, int m) {
             const int r = m0 + m * 32 + j;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x[m][c] = xs[b][r * 8 + ((2 * c + h) ^ (r & 7))];
-            s[m] = sxs[b][r] * sws[wn][kb];
+            for (int c = 0; c < 4; ++c) x[m][c] = xs[kb & 1][r * 8 + ((2 * c + h) ^ (r >> 1 & 7))];
+        };
+        auto read_w = [&](int kb, int T) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w[T & 1][c] = ws[kb & 1][wn * 1024 + ((2 * T + (j >> 4)) * 2 + (c >> 1)) * 64 + ((2 * c + h) & 3) * 16 + (j & 15)];
+        };
+        auto add = [&](int p, const v16f& from, float scale, int half) {     // half of product p to its sums
+#pragma unroll
+            for (int e = 8 * half; e < 8 * half + 8; ++e) acc[p % MT][p / MT][e] = fmaf(from[e], scale, acc[p % MT][p / MT][e]);
+        };
+        read_w(0, 0);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            read_x(0, m);
+            s[m] = scale_of(0, m0 + m * 32 + j);
         }
-        if ((A.K & 15) && kb == A.KB - 1) {                                  // what stands behind a row's end takes no part
+        all_stages([&](int kb, auto more, auto request) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int left = A.K - kb * SBLOCK - (2 * c + h) * 16 - 4 * q;
-                    const int mask = left >= 4 ? -1 : left <= 0 ? 0 : (1 << (8 * left)) - 1;
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) x[m][c][q] &= mask;
+            for (int p = 0; p < P; ++p) {
+                const int T = p / MT, m = p % MT, last = (p + P - 1) % P;
+                const float scale = p == 0 ? s_last : s[last % MT];
+                if (m == 0 && T < 3) read_w(kb, T + 1);
+                if (m == 0 && T == 3 && more) {
+                    landed();
+                    read_w(kb + 1, 0);
                 }
-        }
+                __builtin_amdgcn_sched_barrier(0);
+                d[p & 1] = half_product<EXACT, 0>(w[T & 1], x[m], (v16f){});
+                add(last, d[(p & 1) ^ 1], scale, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                d[p & 1] = half_product<EXACT, 1>(w[T & 1], x[m], d[p & 1]);
+                add(last, d[(p & 1) ^ 1], scale, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (T == 3 && more) {
+                    if (m == MT - 1) s_last = s[m];
+                    read_x(kb + 1, m);
+                    s[m] = scale_of(kb + 1, m0 + m * 32 + j);
+                    if (request) {
 #pragma unroll
-        for (int T = 0; T < 4; ++T) {
-            v4i w[4];
+                        for (int i = m * XL / MT; i < (m + 1) * XL / MT; ++i) request_x(kb + 2, i);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) w[c] = ws[b][wn * 1024 + ((2 * T + (j >> 4)) * 2 + (c >> 1)) * 64 + ((2 * c + h) & 3) * 16 + (j & 15)];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const v16f d = product32<EXACT>(w, x[m]);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[m][T][e] = fmaf(d[e], s[m], acc[m][T][e]);
+                        for (int i = m * WL / MT; i < (m + 1) * WL / MT; ++i) request_w(kb + 2, i);
+                        if (m == 0) request_s(kb + 2);
+                    }
+                }
             }
+        }, [&](int left) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) cut(x[m][c], left - (2 * c + h) * 16);
+        });
+        add(P - 1, d[(P - 1) & 1], s[MT - 1], 0);
+        add(P - 1, d[(P - 1) & 1], s[MT - 1], 1);
+        if (nb >= A.NB) return;
+        // result e of the T-th instruction is its row 8 (e / 4) + 4 h + e % 4: of the outputs, with output_of, number 4 (2 (T % 2) + e / 8) + e % 4 of
+        // run 2 (e / 4 % 2) + h of 16, in half T / 2 of the block
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float v[64];
+#pragma unroll
+            for (int T = 0; T < 4; ++T)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[((T >> 1) * 2 + (e >> 2 & 1)) * 16 + ((T & 1) * 2 + (e >> 3)) * 4 + (e & 3)] = acc[m][T][e];
+            finish<YT, 4, 32>(A, v, nb, row0 + m0 + m * 32 + j, [&](int i) { return (i >> 1) * 64 + (2 * (i & 1) + h) * 16; });
         }
-    }
-    if (nb >= A.NB) return;
-    // result e of the T-th instruction is its row 8 (e / 4) + 4 h + e % 4: of the outputs, with output_of, number 4 (2 (T % 2) + e / 8) + e % 4 of
-    // run 2 (e / 4 % 2) + h of 16, in half T / 2 of the block
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        float v[64];
-#pragma unroll
-        for (int T = 0; T < 4; ++T)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[((T >> 1) * 2 + (e >> 2 & 1)) * 16 + ((T & 1) * 2 + (e >> 3)) * 4 + (e & 3)] = acc[m][T][e];
-        finish<4, 32>(A, v, nb, row0 + m0 + m * 32 + j, [&](int i) { return (i >> 1) * 64 + (2 * (i & 1) + h) * 16; });
     }
 }
 
-template <bool EXACT, int MT, int WM, int WN>
+template <int YT, int MT, int WM, int WN>
 int launch_tiles(const LinearArgs& A, hipStream_t st)
 {
     constexpr int TM = 32 * MT * WM;
     const int tiles_m = (int)(((long long)A.M + TM - 1) / TM), tiles_n = (A.NB + WN - 1) / WN;
     const long long blocks = ((long long)tiles_m * tiles_n + 7) / 8 * 8;
     if (blocks * WM * WN * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
-    hipLaunchKernelGGL((tile_kernel<EXACT, MT, WM, WN>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, tiles_m, tiles_n, FastDiv(GROUP_M * tiles_n));
+    hipLaunchKernelGGL((tile_kernel<YT, MT, WM, WN>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, tiles_m, tiles_n, FastDiv(GROUP_M * tiles_n));
+    HIP_TRY(hipGetLastError());
+    return MIXAQ_OK;
+}
+
+template <int YT>
+int launch_linear(const LinearArgs& A, hipStream_t st)
+{
+    if ((long long)((A.M + 255) / 256) * ((A.NB + 1) / 2) >= 256 && A.KB >= 4 && A.ldx < (1 << 22)) {
+        if constexpr (exact_sums(YT)) return launch_tiles<YT, 1, 8, 1>(A, st);
+        else return launch_tiles<YT, 2, 4, 2>(A, st);
+    }
+    hipLaunchKernelGGL(linear_kernel<YT>, dim3(A.tiles), dim3(256), 0, st, A);
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
 }
@@ -487,13 +648,12 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
         rc = launch_quantize(*x, rows, K, 1, codes, st);
         if (rc) return rc;
     }
-    const bool exact = y->type == MIXAQ_F32 || y->type == MIXAQ_E4M3;
-    if ((long long)((rows + 255) / 256) * ((h->NB + 1) / 2) >= 256 && h->KB >= 4 && A.ldx < (1 << 22))
-        return exact ? launch_tiles<true, 1, 8, 1>(A, st) : launch_tiles<false, 2, 4, 2>(A, st);
-    if (exact) hipLaunchKernelGGL(linear_kernel<true>, dim3(A.tiles), dim3(256), 0, st, A);
-    else hipLaunchKernelGGL(linear_kernel<false>, dim3(A.tiles), dim3(256), 0, st, A);
-    HIP_TRY(hipGetLastError());
-    return MIXAQ_OK;
+    switch (y->type) {
+    case MIXAQ_F32: return launch_linear<MIXAQ_F32>(A, st);
+    case MIXAQ_F16: return launch_linear<MIXAQ_F16>(A, st);
+    case MIXAQ_BF16: return launch_linear<MIXAQ_BF16>(A, st);
+    default: return launch_linear<MIXAQ_E4M3>(A, st);
+    }
 }
 
 }  // extern "C"
