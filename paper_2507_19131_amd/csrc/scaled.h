@@ -94,12 +94,11 @@ __device__ __forceinline__ BlockScale block_scale(unsigned largest)
     if (largest >= 0x7f800000u) s.scale = s.inv = __uint_as_float(0x7fc00000u);
     return s;
 }
-// four codes, the first in the low byte.  v * inv may pass 448 by its rounding: clamped, as the conversion would make it a NaN.
+// four codes, the first in the low byte.  v * inv may pass 448 by its roundings, by 2^-22 of it: the nearest code is 448 all the same.
 __device__ __forceinline__ int codes4(float a, float b, float c, float d, float inv)
 {
-    const auto q = [&](float v) { return __builtin_amdgcn_fmed3f(v * inv, -E4M3_MAX, E4M3_MAX); };
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q(a), q(b), 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(q(c), q(d), w, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
     return inv == inv ? w : 0x7f7f7f7f;
 }
 template <bool TINY>
@@ -122,14 +121,15 @@ __device__ __forceinline__ unsigned over16(unsigned v, Op op)         // of 16 l
     return op(v, dpp<0x140>(v));                                      // eights, by the mirror of 16
 }
 template <typename Op>
-__device__ __forceinline__ unsigned over64(unsigned v, Op op)
+__device__ __forceinline__ unsigned over4rows(unsigned v, Op op)      // of the four lanes l, l + 16, l + 32, l + 48
 {
-    v = over16(v, op);
     const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
     v = op(a[0], a[1]);
     const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
     return op(b[0], b[1]);
 }
+template <typename Op>
+__device__ __forceinline__ unsigned over64(unsigned v, Op op) { return over4rows(over16(v, op), op); }
 struct MaxOf { __device__ unsigned operator()(unsigned a, unsigned b) const { return max(a, b); } };
 struct SumOf { __device__ unsigned operator()(unsigned a, unsigned b) const { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); } };
 __device__ __forceinline__ unsigned max16(unsigned m) { return over16(m, MaxOf()); }

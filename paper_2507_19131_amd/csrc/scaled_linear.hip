@@ -29,7 +29,7 @@ namespace {
     } while (0)
 
 struct LinearArgs {
-    const uint8_t* x;                 // codes
+    const uint8_t* x;                 // codes (split_kernel: or values)
     const float* sx;
     const uint8_t* w;
     const float* sw;
@@ -37,8 +37,7 @@ struct LinearArgs {
     void* y;
     float* sy;
     long long ldx, ldsx, ldy, ldsy;
-    int M, N, K, KB, NB, y_type, gelu, tiles;
-    FastDiv by_NB;
+    int M, N, K, KB, NB, gelu;
 };
 
 // ---- layouts --------------------------------------------------------------------------------------------------------
@@ -71,18 +70,20 @@ __global__ __launch_bounds__(256) void pack_vectors_kernel(const float* s, long 
 }
 
 // ---- the end of a tile ------------------------------------------------------------------------------------------------
-// GELU(v) = max(v, 0) - |v| erfc(|v| / sqrt 2) / 2, the erfc by Abramowitz and Stegun 7.1.26 (at most 1.5e-7 off): no
-// difference of near values, as 1 + erf would be for negative v.  From |v| = 30 on the second term is 0; a NaN stays one.
+// GELU(v) = v Phi(v), Phi(v) = 1 / (1 + 2^-t), t = v P(v^2): the logarithm of Phi's odds is odd and smooth, P its fit by weighted least
+// squares on 0 < v < 7 (at most 9.4e-8 |v| off; beyond, t only grows).  19 issue slots with the two quarter-rate instructions at four each;
+// by Abramowitz and Stegun's erfc, which is as exact, 25.  The maximum keeps the last product at -infinity from being 0 times infinity; a NaN
+// comes through the other factor.
 __device__ __forceinline__ float gelu(float v)
 {
-    const float a = fminf(fabsf(v), 30.0f), z = a * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.0f));
-    float p = fmaf(t, 1.061405429f, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f);
-    const float e = __builtin_amdgcn_exp2f(z * z * -1.44269504f);
-    return (v < 0.0f ? 0.0f : v) - 0.5f * a * (p * t * e);
+    const float u = v * v;
+    float p = fmaf(u, 0x1.67ab6cp-28f, -0x1.9e7b64p-22f);
+    p = fmaf(p, u, 0x1.80c28cp-17f);
+    p = fmaf(p, u, -0x1.4e76fep-13f);
+    p = fmaf(p, u, -0x1.8fb242p-14f);
+    p = fmaf(p, u, 0x1.ad6ad0p-4f);
+    p = fmaf(p, u, 0x1.26aebcp+1f);
+    return fmaxf(v, -0x1.fffffep+127f) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * p));
 }
 
 // The outputs of one row that a lane holds: RUNS runs of 16 neighbouring ones, run i from column offset(i) of block nb on; the lanes
@@ -197,27 +198,164 @@ __device__ __forceinline__ v4f product(v4i w0, v4i w1, v4i x0, v4i x1)
     }
 }
 
-// A wave per 16 rows and 128 outputs, operands straight from memory.
-template <int YT>
-__global__ __launch_bounds__(256) void linear_kernel(LinearArgs A)
+// ---- operands straight from memory, K split over the waves --------------------------------------------------------------------
+// A workgroup of NW waves computes 16 MR rows times NR tiles of 16 outputs, wave w the blocks w, w + NW, .. of K; the waves' sums meet in LDS,
+// in the order of the waves.  For products of few tiles: a lone row at K = 1024 is one round trip to memory.  A block's scale meets
+// its product where both are of one row, so x may be given as values: a lane holds 32 of the 128 values of its row, the other three
+// lanes of the row the rest, and what it needs as operand is the codes of its own.
+template <int XT>
+__device__ __forceinline__ void operand_of(const LinearArgs& A, int row, int kb, int g, v4i (&x)[2], float& scale)
 {
-    const int lane = threadIdx.x & 63, g = lane >> 4;
-    const int rt = A.by_NB(blockIdx.x), nb = blockIdx.x - rt * A.NB;
-    const int row = rt * 64 + (threadIdx.x >> 6) * 16 + (lane & 15), r = min(row, A.M - 1);
-    float v[32] = {};
-    for (int kb = 0; kb < A.KB; ++kb) {
-        const uint8_t* xr = A.x + r * A.ldx;
-        const v4i x0 = load_codes(xr, kb * SBLOCK + g * 16, A.K), x1 = load_codes(xr, kb * SBLOCK + 64 + g * 16, A.K);
-        const float s = A.sx[kb * A.ldsx + r] * A.sw[kb * A.NB + nb];
-        const v4i* w = (const v4i*)(A.w + ((long long)nb * A.KB + kb) * 8 * TILE_BYTES) + lane;
+    const int k0 = kb * SBLOCK + g * 16;
+    if constexpr (XT == MIXAQ_E4M3) {
+        const uint8_t* const from = A.x + (long long)row * A.ldx;
+        if ((kb + 1) * SBLOCK <= A.K) {
+            x[0] = *(const v4i*)(from + k0);
+            x[1] = *(const v4i*)(from + k0 + 64);
+        } else {
+            x[0] = load_codes(from, k0, A.K);
+            x[1] = load_codes(from, k0 + 64, A.K);
+        }
+        scale = A.sx[kb * A.ldsx + row];
+    } else {
+        using T = typename TypeOf<XT>::T;
+        const T* const from = (const T*)A.x + (long long)row * A.ldx;
+        T t[2][16];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const v4f d = product<exact_sums(YT)>(w[t * 128], w[t * 128 + 64], x0, x1);
+        for (int h = 0; h < 2; ++h) {
+            if ((kb + 1) * SBLOCK <= A.K) __builtin_memcpy(t[h], from + k0 + h * 64, sizeof(t[h]));
+            else
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[t * 4 + e] = fmaf(d[e], s, v[t * 4 + e]);
+                for (int e = 0; e < 16; ++e) t[h][e] = k0 + h * 64 + e < A.K ? from[k0 + h * 64 + e] : (T)0.0f;
+        }
+        unsigned largest = 0;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) largest = max(largest, magnitude((float)t[e >> 4][e & 15]));
+        const BlockScale s = block_scale(over4rows(largest, MaxOf()));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[h][q] = codes4((float)t[h][4 * q], (float)t[h][4 * q + 1], (float)t[h][4 * q + 2], (float)t[h][4 * q + 3], s.inv);
+        scale = s.scale;
+    }
+}
+
+template <int XT, int YT, int MR, int NR, int NW>
+__global__ __launch_bounds__(NW * 64) void split_kernel(LinearArgs A, int row_tiles, FastDiv by_rows, int groups)
+{
+    constexpr bool EXACT = exact_sums(YT);
+    constexpr int FR = MR * NR;                                              // 16 x 16 results of the workgroup
+    __shared__ v4f part[NW][FR][64];
+    __shared__ unsigned top[YT == MIXAQ_E4M3 ? FR : 1][16];
+    static_assert(YT != MIXAQ_E4M3 || NR == 8, "a row's codes need its whole block");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    // a run of workgroups per XCD, the row tiles of one run of weights beside one another
+    const int per_xcd = (groups + 7) / 8, t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per_xcd || t >= groups) return;            // the whole workgroup
+    const int nt = by_rows(t), rt = t - nt * row_tiles, nb = nt * NR / 8, tile0 = nt * NR % 8;
+    if (nb * SBLOCK + output_of(tile0, 0) >= A.N) return;                    // (the tiles of the last block may all lie beyond)
+    int row[MR];
+#pragma unroll
+    for (int m = 0; m < MR; ++m) row[m] = min(rt * 16 * MR + m * 16 + c, A.M - 1);
+    v4f acc[MR][NR] = {};
+    struct Operands {
+        v4i x[MR][2], w[NR][2];
+        float s[MR];
+    };
+    auto load = [&](int kb, Operands& o) {
+        const v4i* const w = (const v4i*)(A.w + (((long long)nb * A.KB + kb) * 8 + tile0) * TILE_BYTES) + lane;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            o.w[n][0] = w[n * 128];
+            o.w[n][1] = w[n * 128 + 64];
+        }
+        const float sw = A.sw[kb * A.NB + nb];
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+            operand_of<XT>(A, row[m], kb, g, o.x[m], o.s[m]);
+            o.s[m] *= sw;
+        }
+    };
+    auto multiply = [&](const Operands& o) {
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+                const v4f d = product<EXACT>(o.w[n][0], o.w[n][1], o.x[m][0], o.x[m][1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[m][n][e] = fmaf(d[e], o.s[m], acc[m][n][e]);
+            }
+    };
+    if (wave < A.KB) {                                                       // one block's operands travel under the products of the last one
+        Operands now;
+        load(wave, now);
+        for (int kb = wave + NW; kb < A.KB; kb += NW) {
+            Operands next;
+            load(kb, next);
+            multiply(now);
+            now = next;
+        }
+        multiply(now);
+    }
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int n = 0; n < NR; ++n) part[wave][m * NR + n][lane] = acc[m][n];
+    __syncthreads();
+    constexpr int MINE = (FR + NW - 1) / NW;                                 // results that a wave sums and finishes
+    v4f y[MINE];
+    const int used = min(NW, A.KB);
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        const int f = wave + i * NW;
+        if (f >= FR) break;
+        v4f v = part[0][f][lane];
+        for (int w = 1; w < used; ++w) v += part[w][f][lane];
+        const int n0 = nb * SBLOCK + output_of(tile0 + f % NR, 4 * g);
+        v4f b;
+        __builtin_memcpy(&b, A.bias + n0, sizeof(b));
+        v += b;
+        if (A.gelu) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = gelu(v[e]);
+        }
+        y[i] = v;
+        if constexpr (YT == MIXAQ_E4M3) {
+            unsigned m = 0;                                                  // (outputs beyond N are gelu(0) = 0, or NaN where the whole row is)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = max(m, magnitude(v[e]));
+            m = over4rows(m, MaxOf());
+            if (g == 0) top[f][c] = m;
         }
     }
-    finish<YT, 2, 16>(A, v, nb, row, [&](int i) { return i * 64 + g * 16; });
+    if constexpr (YT == MIXAQ_E4M3) __syncthreads();
+    using T = typename TypeOf<YT>::T;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        const int f = wave + i * NW;
+        if (f >= FR) break;
+        const int r = rt * 16 * MR + f / NR * 16 + c, n0 = nb * SBLOCK + output_of(tile0 + f % NR, 4 * g);
+        T out[4];
+        if constexpr (YT == MIXAQ_E4M3) {
+            unsigned m = 0;
+#pragma unroll
+            for (int n = 0; n < NR; ++n) m = max(m, top[f / NR * NR + n][c]);
+            const BlockScale s = block_scale(m);
+            const int w = codes4(y[i][0], y[i][1], y[i][2], y[i][3], s.inv);
+            __builtin_memcpy(out, &w, 4);
+            if (r < A.M && g == 0 && f % NR == 0) A.sy[nb * A.ldsy + r] = s.scale;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = (T)y[i][e];
+        }
+        if (r >= A.M) continue;
+        T* const to = (T*)A.y + (long long)r * A.ldy + n0;
+        if (n0 + 4 <= A.N) __builtin_memcpy(to, out, sizeof(out));
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n0 + e < A.N) to[e] = out[e];
+    }
 }
 
 // ---- both operands through LDS ------------------------------------------------------------------------------------------
@@ -517,25 +655,60 @@ int launch_tiles(const LinearArgs& A, hipStream_t st)
     return MIXAQ_OK;
 }
 
-template <int YT>
-int launch_linear(const LinearArgs& A, hipStream_t st)
+template <int XT, int YT, int MR, int NR, int NW>
+int launch_split(const LinearArgs& A, hipStream_t st)
 {
-    if ((long long)((A.M + 255) / 256) * ((A.NB + 1) / 2) >= 256 && A.KB >= 4 && A.ldx < (1 << 22)) {
+    const long long row_tiles = ((long long)A.M + 16 * MR - 1) / (16 * MR), groups = row_tiles * (A.NB * 8 / NR);
+    const long long blocks = (groups + 7) / 8 * 8;
+    if (blocks * NW * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
+    hipLaunchKernelGGL((split_kernel<XT, YT, MR, NR, NW>), dim3((unsigned)blocks), dim3(NW * 64), 0, st, A, (int)row_tiles, FastDiv((int)row_tiles), (int)groups);
+    HIP_TRY(hipGetLastError());
+    return MIXAQ_OK;
+}
+
+// Which kernel takes a product: by rows, K and N alone, so that the sums are the same whatever the types of x and y.
+enum Form { FORM_FEW, FORM_SPLIT, FORM_TILE, FORM_LARGE };
+Form form_of(int M, const mixaq_scaled_linear* h, long long ldx)
+{
+    const long long tiles128 = (M + 127LL) / 128 * h->NB, tiles256 = (M + 255LL) / 256 * ((h->NB + 1) / 2);
+    if (M <= 64) return FORM_FEW;
+    if (ldx >= (1 << 22)) return FORM_SPLIT;
+    if (tiles256 >= 256 && h->KB >= 4) return FORM_LARGE;
+    return tiles128 >= 256 ? FORM_TILE : FORM_SPLIT;
+}
+
+template <int XT, int YT>
+int launch_few(const LinearArgs& A, hipStream_t st)
+{
+    if constexpr (YT == MIXAQ_E4M3) return launch_split<XT, YT, 1, 8, 8>(A, st);
+    else return launch_split<XT, YT, 1, 1, 8>(A, st);
+}
+template <int YT>
+int launch_linear(const LinearArgs& A, Form form, int x_type, hipStream_t st)
+{
+    switch (form) {
+    case FORM_FEW:
+        if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT>(A, st);
+        if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT>(A, st);
+        if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT>(A, st);
+        return launch_few<MIXAQ_E4M3, YT>(A, st);
+    case FORM_SPLIT:
+        if constexpr (YT == MIXAQ_E4M3) return launch_split<MIXAQ_E4M3, YT, 2, 8, 4>(A, st);
+        else return launch_split<MIXAQ_E4M3, YT, 4, 4, 4>(A, st);
+    case FORM_TILE: return launch_tiles<YT, 1, 4, 1>(A, st);
+    default:
         if constexpr (exact_sums(YT)) return launch_tiles<YT, 1, 8, 1>(A, st);
         else return launch_tiles<YT, 2, 4, 2>(A, st);
     }
-    hipLaunchKernelGGL(linear_kernel<YT>, dim3(A.tiles), dim3(256), 0, st, A);
-    HIP_TRY(hipGetLastError());
-    return MIXAQ_OK;
 }
 
 int round_up16(int v) { return (v + 15) / 16 * 16; }
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// the workspace: codes and scales of x, where it is given as values
+// the workspace: codes and scales of x, where it is given as values and not quantized on its way into the product
 size_t workspace_of(const mixaq_scaled_linear* h, int32_t rows, int32_t x_type)
 {
-    if (x_type == MIXAQ_E4M3 || rows == 0) return 0;
+    if (x_type == MIXAQ_E4M3 || rows == 0 || form_of(rows, h, 0) == FORM_FEW) return 0;
     return align256((size_t)rows * round_up16(h->d.K)) + align256((size_t)rows * h->KB * 4);
 }
 
@@ -639,20 +812,19 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
     A.y = y->data; A.ldy = y->stride;
     A.sy = y->scales; A.ldsy = y->scale_stride;
     A.M = rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
-    A.y_type = y->type; A.gelu = h->d.activation == 1;
-    A.by_NB = FastDiv(h->NB);
-    const long long tiles = (long long)((rows + 63LL) / 64) * h->NB;
-    if (tiles * 256 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", rows, N);
-    A.tiles = (int)tiles;
+    A.gelu = h->d.activation == 1;
+    const Form form = form_of(rows, h, A.ldx);
+    int x_type = x->type;
     if (need) {
         rc = launch_quantize(*x, rows, K, 1, codes, st);
         if (rc) return rc;
+        x_type = MIXAQ_E4M3;
     }
     switch (y->type) {
-    case MIXAQ_F32: return launch_linear<MIXAQ_F32>(A, st);
-    case MIXAQ_F16: return launch_linear<MIXAQ_F16>(A, st);
-    case MIXAQ_BF16: return launch_linear<MIXAQ_BF16>(A, st);
-    default: return launch_linear<MIXAQ_E4M3>(A, st);
+    case MIXAQ_F32: return launch_linear<MIXAQ_F32>(A, form, x_type, st);
+    case MIXAQ_F16: return launch_linear<MIXAQ_F16>(A, form, x_type, st);
+    case MIXAQ_BF16: return launch_linear<MIXAQ_BF16>(A, form, x_type, st);
+    default: return launch_linear<MIXAQ_E4M3>(A, form, x_type, st);
     }
 }
 

@@ -80,7 +80,7 @@ def linear(x, w, bias, with_gelu, kind):
         bound = bound + 7 * 2.0 ** -13 * (top(x) @ top(w).T)
     if not with_gelu:
         return y, bound
-    # |gelu'| < 1.13; the erfc's 1.5e-7 times |v| / 2, its factors' roundings (exponent: v^2 / 2 * 2 U, at most 0.17 |v| of it left), the sum's
+    # |gelu'| < 1.13; an approximation of Phi to 0.75e-7 (relative to v), and the roundings of its steps
     return gelu(y), 1.13 * bound + np.abs(y) * (0.75e-7 + 16 * U)
 
 

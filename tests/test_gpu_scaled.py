@@ -253,8 +253,9 @@ def test_gelu_far_from_zero():
 
 def test_layer_refuses():
     with Layer(3, 100, 200) as layer:
-        x, y = placed(values(1, 8, 200), "bf16"), Room(8, 100, "f32")
-        ws = M.alloc_linear_workspace(layer.h, 8, torch.bfloat16, torch.float32)
+        x, y = placed(values(1, 80, 200), "bf16"), Room(80, 100, "f32")
+        ws = M.alloc_linear_workspace(layer.h, 80, torch.bfloat16, torch.float32)
+        assert ws.numel() and M.mixaq_scaled_linear_workspace_bytes(layer.h, 8, torch.bfloat16, torch.float32) == 0
         call = M.mixaq_scaled_linear_forward
 
         def refused(code, words, *a, **kw):
@@ -266,16 +267,16 @@ def test_layer_refuses():
         refused(-4, "needed", x.t, y.t, workspace=ws[:-1])
         refused(-4, "aligned", x.t, y.t, workspace=torch.empty(ws.numel() + 256, dtype=torch.uint8, device="cuda")[16:])
         refused(-2, "overlap", x.t, x.t[:, :100], workspace=ws)
-        large = torch.zeros(8192, dtype=torch.uint8, device="cuda")
-        refused(-2, "workspace overlaps", large.view(torch.bfloat16)[:1600].view(8, 200), y.t, workspace=large)
+        large = torch.zeros(65536, dtype=torch.uint8, device="cuda")
+        refused(-2, "workspace overlaps", large.view(torch.bfloat16)[:16000].view(80, 200), y.t, workspace=large)
         with pytest.raises(ValueError, match="do not fit"):
             call(layer.h, x.t[:, :199], y.t, workspace=ws)
         with pytest.raises(ValueError, match="scales"):
-            call(layer.h, Room(8, 200, "e4m3").t, y.t, workspace=ws)
+            call(layer.h, Room(80, 200, "e4m3").t, y.t, workspace=ws)
         with pytest.raises(ValueError, match="scales"):
-            call(layer.h, x.t, y.t, x_scales=torch.ones((2, 8), device="cuda"), workspace=ws)
+            call(layer.h, x.t, y.t, x_scales=torch.ones((2, 80), device="cuda"), workspace=ws)
         call(layer.h, x.t[:0], y.t[:0])                         # nothing to do
-        wide = torch.zeros((8, 512), dtype=torch.bfloat16, device="cuda")
+        wide = torch.zeros((80, 512), dtype=torch.bfloat16, device="cuda")
         call(layer.h, wide[:, :200], wide[:, 200:300], workspace=ws)     # columns of one matrix are no overlap
 
 
