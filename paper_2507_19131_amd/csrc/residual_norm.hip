@@ -30,7 +30,7 @@ struct NormArgs {
 // Sum over the G lanes of a row; with more than a wave, through LDS (`part`: twice a float per wave, used in turn, so that one barrier is
 // enough: who writes a half again has passed the barrier of the other one, behind which nobody reads it any more).
 template <int G>
-__device__ __forceinline__ float row_sum(float v, float (*part)[4], int& turn)
+__device__ __forceinline__ float row_sum(float v, float (*part)[G / 64 + 1], int& turn)
 {
     if constexpr (G == 16) return __uint_as_float(over16(__float_as_uint(v), SumOf()));
     v = __uint_as_float(over64(__float_as_uint(v), SumOf()));
@@ -39,7 +39,9 @@ __device__ __forceinline__ float row_sum(float v, float (*part)[4], int& turn)
         turn ^= 1;
         if ((threadIdx.x & 63) == 0) p[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = (p[0] + p[1]) + (p[2] + p[3]);
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < G / 64; w += 4) v += (p[w] + p[w + 1]) + (p[w + 2] + p[w + 3]);
     }
     return v;
 }
@@ -51,7 +53,7 @@ __device__ __forceinline__ void load_vector(Vector<V>& to, const float* from, co
 {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        if (from) load8<TINY>(from, c[j], C, to.v[j]);
+        if (from) load8f<TINY>(from, c[j], C, to.v[j]);
         else
 #pragma unroll
             for (int e = 0; e < 8; ++e) to.v[j][e] = otherwise;
@@ -62,7 +64,7 @@ __device__ __forceinline__ void load_vector(Vector<V>& to, const float* from, co
 // a large mean costs no digits.  Sums in binary32.
 template <int G, int V, bool TINY>
 __device__ __forceinline__ void norm_row(float (&v)[V][8], int kind, float eps, const Vector<V>& gamma, const Vector<V>& beta, const Eight (&c)[V],
-                                         const NormArgs& A, float (*part)[4], int& turn)
+                                         const NormArgs& A, float (*part)[G / 64 + 1], int& turn)
 {
     float mean = 0.0f;
     if (kind == NORM_LAYER) {
@@ -89,21 +91,25 @@ __device__ __forceinline__ void norm_row(float (&v)[V][8], int kind, float eps, 
         for (int e = 0; e < 8; ++e) v[j][e] = fmaf(v[j][e] * r, gamma.v[j][e], beta.v[j][e]);
 }
 
-// KEEP: the vectors of both norms stay in registers from row to row; else they come anew (from the caches) for every row, where V times eight
-// values of four of them would not fit beside the row.
+// A workgroup's next row is on its way while this one is worked on: with about three workgroups a CU, whose rows would otherwise be
+// requested, reduced and stored in turn, memory is seldom without requests.  KEEP: the vectors of both norms and the gate stay in registers
+// from row to row; else they come anew (from the caches) for every row, where four of them would not fit beside it.
+// What bounds it is memory: 8190 x 4096 of bf16 with two outputs 4.4 TB/s, a copy of that size 5.1.  Rows that start anywhere (an
+// odd width) cost a third more: every vector access of a wave then touches a line more.
 template <int TX, int TB, int G, int V, bool TINY>
-__global__ __launch_bounds__(256) void residual_norm_kernel(NormArgs A)
+__global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormArgs A)
 {
     using X = typename TypeOf<TX>::T;
     using B = typename TypeOf<TB>::T;
-    constexpr bool KEEP = V <= 2;
-    __shared__ float part[2][4];
+    constexpr bool KEEP = G <= 256 || V == 1;
+    constexpr int ROWS = G < 256 ? 256 / G : 1;                       // at one time
+    __shared__ float part[2][G / 64 + 1];
     int turn = 0;
-    const int l = threadIdx.x % G, rows_at_once = 256 / G;
+    const int l = threadIdx.x % G;
     Eight c[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) c[j] = place8<TINY>((j * G + l) * 8, A.C);
-    Vector<V> post_gamma, post_beta, pre_gamma, pre_beta;
+    Vector<V> post_gamma, post_beta, pre_gamma, pre_beta, gate;
     auto load_post = [&] {
         load_vector<G, V, TINY>(post_gamma, A.post_gamma, c, A.C, 1.0f);
         load_vector<G, V, TINY>(post_beta, A.post_beta, c, A.C, 0.0f);
@@ -112,38 +118,51 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(NormArgs A)
         load_vector<G, V, TINY>(pre_gamma, A.pre_gamma, c, A.C, 1.0f);
         load_vector<G, V, TINY>(pre_beta, A.pre_beta, c, A.C, 0.0f);
     };
-    if (KEEP && A.post) load_post();
-    if (KEEP && A.pre) load_pre();
-    for (long long r0 = (long long)blockIdx.x * rows_at_once; r0 < A.rows; r0 += (long long)gridDim.x * rows_at_once) {
-        const long long row = r0 + threadIdx.x / G;
-        const bool real = row < A.rows;
-        const long long at = real ? row : A.rows - 1;                // spare lanes take the last row along and store nothing
-        float x[V][8], y[V][8], gate[V][8];
+    const long long step = (long long)gridDim.x * ROWS;
+    long long row = (long long)blockIdx.x * ROWS + threadIdx.x / G;
+    X tx[V][8];
+    B tb[V][8];
+    auto request = [&](long long r) {
+        const long long at = min(r, (long long)A.rows - 1);          // spare lanes take the last row along and store nothing
 #pragma unroll
-        for (int j = 0; j < V; ++j) load8<TINY>((const X*)A.x + at * A.ldx, c[j], A.C, x[j]);
+        for (int j = 0; j < V; ++j) load8<TINY>((const X*)A.x + at * A.ldx, c[j], A.C, tx[j]);
         if (A.branch) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) load8<TINY>((const B*)A.branch + at * A.ldb, c[j], A.C, y[j]);
-            if (A.gate) {
-                const float* from = A.gate + (long long)((int)at / A.rows_per_gate) * A.C;
+            for (int j = 0; j < V; ++j) load8<TINY>((const B*)A.branch + at * A.ldb, c[j], A.C, tb[j]);
+        }
+    };
+    request(row);
+    if (KEEP && A.post) load_post();
+    if (KEEP && A.pre) load_pre();
+    int gate_row = -1;
+    for (long long r0 = row - threadIdx.x / G; r0 < A.rows; r0 += step, row += step) {
+        const bool real = row < A.rows;
+        float x[V][8], y[V][8];
 #pragma unroll
-                for (int j = 0; j < V; ++j) load8<TINY>(from, c[j], A.C, gate[j]);
-            }
-            if (A.post) {
-                if (!KEEP) load_post();
-                norm_row<G, V, TINY>(y, A.post, A.post_eps, post_gamma, post_beta, c, A, part, turn);
-            }
-            if (A.gate) {
+        for (int j = 0; j < V; ++j)
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[j][e] *= gate[j][e];
+            for (int e = 0; e < 8; ++e) {
+                x[j][e] = (float)tx[j][e];
+                y[j][e] = A.branch ? (float)tb[j][e] : 0.0f;
             }
+        // (of rows written in place too: another turn's row is another row, and what spare lanes read nobody uses)
+        if (r0 + step < A.rows) request(row + step);
+        if (A.gate) {
+            const int g = (int)min(row, (long long)A.rows - 1) / A.rows_per_gate;
+            if (!KEEP || g != gate_row) load_vector<G, V, TINY>(gate, A.gate + (long long)g * A.C, c, A.C, 1.0f);
+            gate_row = g;
+        }
+        if (A.post) {
+            if (!KEEP) load_post();
+            norm_row<G, V, TINY>(y, A.post, A.post_eps, post_gamma, post_beta, c, A, part, turn);
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[j][e] = A.branch ? fmaf(A.residual_scale, x[j][e], y[j][e]) : A.residual_scale * x[j][e];
+            for (int e = 0; e < 8; ++e) {
+                if (A.gate) y[j][e] *= gate.v[j][e];
+                y[j][e] = A.branch ? fmaf(A.residual_scale, x[j][e], y[j][e]) : A.residual_scale * x[j][e];
+            }
             if (A.y && real) store8<TINY>((X*)A.y + row * A.ldy, c[j], A.C, y[j]);
         }
         if (!A.out) continue;
@@ -175,11 +194,15 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(NormArgs A)
 template <int TX, int TB, int G, int V, bool TINY = false>
 void launch(const NormArgs& A, hipStream_t st)
 {
-    // as many workgroups as run at one time, each on every so many rows: the vectors are loaded once
-    const long long groups = ((long long)A.rows + 256 / G - 1) / (256 / G);
-    hipLaunchKernelGGL((residual_norm_kernel<TX, TB, G, V, TINY>), dim3((unsigned)std::min(groups, 2048LL)), dim3(256), 0, st, A);
+    // Three workgroups a CU, each on every 768th group of rows: neighbouring rows are on their way at one time.  8190 x 4096 values of bf16 with
+    // gates, us: 512 workgroups 68, 768 61, 1024 73, 2048 67, 4096 71; a run of neighbouring rows for each of 1024 73.
+    constexpr int ROWS = G < 256 ? 256 / G : 1;
+    const long long groups = ((long long)A.rows + ROWS - 1) / ROWS;
+    hipLaunchKernelGGL((residual_norm_kernel<TX, TB, G, V, TINY>), dim3((unsigned)std::min(groups, 768LL)), dim3(G < 256 ? 256 : G), 0, st, A);
 }
-// The lanes of a row: 16 as long as three vectors of eight hold their share, then a wave, then a workgroup.
+// The lanes of a row: 16, a wave, then a workgroup of four or sixteen, with one or two times eight values each.  (us, bf16, with gates:  C = 256
+// in 16 lanes of two 60, in 64 of one 88;  1024 in 64 of two 61, in 256 of one 105;  4096 in 256 of two 60, in 512 of one 71;  8192 in 512 of
+// two 92, in 1024 of one, which can keep the vectors, 82.)
 template <int TX, int TB>
 void launch_types(const NormArgs& A, hipStream_t st)
 {
@@ -190,8 +213,8 @@ void launch_types(const NormArgs& A, hipStream_t st)
     else if (A.C <= 1024) launch<TX, TB, 64, 2>(A, st);
     else if (A.C <= 2048) launch<TX, TB, 256, 1>(A, st);
     else if (A.C <= 4096) launch<TX, TB, 256, 2>(A, st);
-    else if (A.C <= 8192) launch<TX, TB, 256, 4>(A, st);
-    else launch<TX, TB, 256, 8>(A, st);
+    else if (A.C <= 8192) launch<TX, TB, 1024, 1>(A, st);
+    else launch<TX, TB, 1024, 2>(A, st);
 }
 template <int TX>
 void launch_branch(const NormArgs& A, int tb, hipStream_t st)

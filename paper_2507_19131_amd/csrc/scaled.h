@@ -37,15 +37,20 @@ __device__ __forceinline__ Eight place8(int col, int C)
     return {at, min(col - at, 8)};
 }
 template <bool TINY, typename T>
-__device__ __forceinline__ void load8(const T* row, Eight c, int C, float v[8])
+__device__ __forceinline__ void load8(const T* row, Eight c, int C, T t[8])
 {
-    T t[8];
     if constexpr (TINY) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[e] = e < C ? row[e] : (T)0.0f;
     } else {
-        __builtin_memcpy(t, row + c.at, sizeof(t));
+        __builtin_memcpy(t, row + c.at, 8 * sizeof(T));
     }
+}
+template <bool TINY, typename T>
+__device__ __forceinline__ void load8f(const T* row, Eight c, int C, float v[8])
+{
+    T t[8];
+    load8<TINY>(row, c, C, t);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
 }

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs A)
         const Eight c = place8<TINY>(b * SBLOCK + l * 8, A.cols);
         float v[4][8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load8<TINY>((const T*)A.x + (long long)min(rg * 16 + j * 4 + g, A.rows - 1) * A.ldx, c, A.cols, v[j]);
+        for (int j = 0; j < 4; ++j) load8f<TINY>((const T*)A.x + (long long)min(rg * 16 + j * 4 + g, A.rows - 1) * A.ldx, c, A.cols, v[j]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int row = rg * 16 + j * 4 + g;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(QuantArgs A)
     float v[8][8];
     unsigned m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) load8<TINY>((const T*)A.x + (long long)min(tr * SBLOCK + j * 16 + g, A.rows - 1) * A.ldx, c, A.cols, v[j]);
+    for (int j = 0; j < 8; ++j) load8f<TINY>((const T*)A.x + (long long)min(tr * SBLOCK + j * 16 + g, A.rows - 1) * A.ldx, c, A.cols, v[j]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = max(m, max_magnitude<TINY>(c, A.cols, v[j]));        // (the last row once more is no other maximum)
     m = over64(m, MaxOf());
