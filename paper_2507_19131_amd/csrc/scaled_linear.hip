@@ -3,6 +3,7 @@
 #include "scaled.h"
 
 #include <algorithm>
+#include <cmath>
 #include <new>
 #include <type_traits>
 
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(256) void pack_vectors_kernel(const float* s, long 
 // ---- the end of a tile ------------------------------------------------------------------------------------------------
 // GELU(v) = v Phi(v), Phi(v) = 1 / (1 + 2^-t), t = v P(v^2): the logarithm of Phi's odds is odd and smooth, P its fit by weighted least
 // squares on 0 < v < 7 (at most 9.4e-8 |v| off; beyond, t only grows).  19 issue slots with the two quarter-rate instructions at four each;
-// by Abramowitz and Stegun's erfc, which is as exact, 25.  The maximum keeps the last product at -infinity from being 0 times infinity; a NaN
+// by Abramowitz and Stegun's erfc, which is as exact, 25.  The median keeps the last product at -infinity from being 0 times infinity; a NaN
 // comes through the other factor.
 __device__ __forceinline__ float gelu(float v)
 {
@@ -83,86 +84,97 @@ __device__ __forceinline__ float gelu(float v)
     p = fmaf(p, u, -0x1.8fb242p-14f);
     p = fmaf(p, u, 0x1.ad6ad0p-4f);
     p = fmaf(p, u, 0x1.26aebcp+1f);
-    return fmaxf(v, -0x1.fffffep+127f) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * p));
+    return __builtin_amdgcn_fmed3f(v, -0x1.fffffep+127f, INFINITY) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * p));
 }
 
-// The outputs of one row that a lane holds: RUNS runs of 16 neighbouring ones, run i from column offset(i) of block nb on; the lanes
-// l, l + LANE_STEP, .. hold the whole block.  A block inside the matrix takes the short way, the last one stores value by value.
-template <int YT, int RUNS, int LANE_STEP, typename Offset>
-__device__ __forceinline__ void finish(const LinearArgs& A, float (&v)[16 * RUNS], int nb, int row, Offset offset)
+// The end of a wave's ROWS rows and 128 outputs: a lane holds those of one row, the bias in them, in RUNS runs of 16 neighbouring ones, run i from
+// column offset(i) of block nb on; the lanes l, l + ROWS, .. hold the whole row.  Through LDS (`turn`: 16 or 32 rows x 256 bytes of the
+// wave's own), so that a store covers whole lines: from the lanes themselves it would touch 32 rows with 32 bytes each (268 324 x 128 -> 512 of bf16
+// STORES_MEASURED).  Its 16-byte pieces are turned by the row, so that neither side meets a bank twice.  The last block of a row that ends
+// inside it is stored value by value.
+template <int YT, int RUNS, int ROWS, typename Offset>
+__device__ __forceinline__ void finish(const LinearArgs& A, float (&v)[16 * RUNS], int nb, long long row0, v4i* turn, Offset offset)
 {
     using T = typename TypeOf<YT>::T;
-    const int col = nb * SBLOCK;
-    T* const y = (T*)A.y + (long long)min(row, A.M - 1) * A.ldy + col;
-    auto activate = [&](int i) {
-        float b[16];
-        __builtin_memcpy(b, A.bias + col + offset(i), sizeof(b));
+    constexpr int ES = sizeof(T), ROW_BYTES = 128 * ES < 256 ? 128 * ES : 256, PASSES = 128 * ES / ROW_BYTES, PIECES = ROW_BYTES / 16;
+    const int lane = threadIdx.x & 63, own = lane % ROWS, col = nb * SBLOCK;
+    const long long row = row0 + own;
+    if (A.gelu) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[i * 16 + e] += b[e];
-        if (A.gelu) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[i * 16 + e] = gelu(v[i * 16 + e]);
-        }
-    };
-    auto store = [&](int i, const T (&t)[16]) {
-        if (row >= A.M) return;
-        if (col + SBLOCK <= A.N) {
-            __builtin_memcpy(y + offset(i), t, sizeof(t));
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (col + offset(i) + e < A.N) y[offset(i) + e] = t[e];
-        }
-    };
+        for (int e = 0; e < 16 * RUNS; ++e) v[e] = gelu(v[e]);
+    }
+    T t[RUNS][16];
     if constexpr (YT == MIXAQ_E4M3) {
-        unsigned largest = 0;                             // outputs beyond N are gelu(0) = 0 (or NaN where the whole row is)
+        // two maxima of the bits, three values an instruction: of the positive numbers as integers, of the negative ones without a sign
+        int up = 0;
+        unsigned down = 0;
 #pragma unroll
-        for (int i = 0; i < RUNS; ++i) {
-            activate(i);
-            asm volatile("" ::: "memory");                // one run's bias at a time
+        for (int e = 0; e < 16 * RUNS; e += 2) {
+            up = max(max(up, __float_as_int(v[e])), __float_as_int(v[e + 1]));
+            down = max(max(down, __float_as_uint(v[e])), __float_as_uint(v[e + 1]));
         }
+        unsigned largest = max((unsigned)up, (down >> 31) * (down & 0x7fffffffu));       // outputs beyond N are gelu(0) = 0 (or NaN where the row is)
 #pragma unroll
-        for (int e = 0; e < 16 * RUNS; ++e) largest = max(largest, magnitude(v[e]));
-#pragma unroll
-        for (int d = LANE_STEP; d < 64; d <<= 1) largest = max(largest, (unsigned)__shfl_xor((int)largest, d, 64));
+        for (int d = ROWS; d < 64; d <<= 1) largest = max(largest, (unsigned)__shfl_xor((int)largest, d, 64));
         const BlockScale s = block_scale(largest);
-        if (row < A.M && (threadIdx.x & 63) < LANE_STEP) A.sy[nb * A.ldsy + row] = s.scale;
+        if (row < A.M && lane < ROWS) A.sy[nb * A.ldsy + row] = s.scale;
 #pragma unroll
-        for (int i = 0; i < RUNS; ++i) {
-            T t[16];
+        for (int i = 0; i < RUNS; ++i)
 #pragma unroll
             for (int q = 0; q < 16; q += 4) {
                 const int w = codes4(v[i * 16 + q], v[i * 16 + q + 1], v[i * 16 + q + 2], v[i * 16 + q + 3], s.inv);
-                __builtin_memcpy(t + q, &w, 4);
+                __builtin_memcpy(&t[i][q], &w, 4);
             }
-            store(i, t);
-        }
     } else {
 #pragma unroll
-        for (int i = 0; i < RUNS; ++i) {
-            activate(i);
-            T t[16];
+        for (int i = 0; i < RUNS; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) t[e] = (T)v[i * 16 + e];
-            store(i, t);
-            asm volatile("" ::: "memory");
+            for (int e = 0; e < 16; ++e) t[i][e] = (T)v[i * 16 + e];
+    }
+    if (col + SBLOCK > A.N) {
+        if (row >= A.M) return;
+        T* const y = (T*)A.y + row * A.ldy + col;
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (col + offset(i) + e < A.N) y[offset(i) + e] = t[i][e];
+        return;
+    }
+    auto place = [](int r, int p) { return r * PIECES + (PIECES == 16 ? p ^ (r & 15) : p ^ (r >> 1 & 7)); };
+    auto in_order = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };           // among the lanes of the wave, which runs in step
+    uint8_t* const y = (uint8_t*)A.y + (row0 * A.ldy + col) * ES;
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+#pragma unroll
+        for (int i = pass * RUNS / PASSES; i < (pass + 1) * RUNS / PASSES; ++i) {
+            const int p = offset(i) * ES % ROW_BYTES / 16;
+#pragma unroll
+            for (int q = 0; q < ES; ++q) __builtin_memcpy(&turn[place(own, p + q)], (const uint8_t*)t[i] + q * 16, 16);
         }
+        in_order();
+#pragma unroll
+        for (int k = 0; k < ROWS * PIECES / 64; ++k) {
+            const int r = (k * 64 + lane) / PIECES, p = (k * 64 + lane) % PIECES;
+            const v4i piece = turn[place(r, p)];
+            if (row0 + r < A.M) __builtin_memcpy(y + r * A.ldy * ES + pass * ROW_BYTES + p * 16, &piece, 16);
+        }
+        in_order();
     }
 }
 
 // 16 bytes of a row's codes from byte k on; bytes from K on are zero, so that what stands there takes no part (a NaN there, times a zero
 // weight, would).
+__device__ __forceinline__ void cut(v4i& c, int left)      // of the row's bytes from the chunk on
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) c[q] &= left >= 4 * q + 4 ? -1 : left <= 4 * q ? 0 : (1 << (8 * (left - 4 * q))) - 1;
+}
 __device__ __forceinline__ v4i load_codes(const uint8_t* row, int k, int K)
 {
     v4i v = {0, 0, 0, 0};
     if (k < K) v = *(const v4i*)(row + k);
-    if (k + 16 > K) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int left = K - k - 4 * q;
-            v[q] = left >= 4 ? v[q] : left <= 0 ? 0 : v[q] & ((1 << (8 * left)) - 1);
-        }
-    }
+    cut(v, K - k);
     return v;
 }
 
@@ -365,18 +377,14 @@ __global__ __launch_bounds__(NW * 64) void split_kernel(LinearArgs A, int row_ti
 // Rows of x lie in LDS as 8 chunks of 16 bytes whose places are turned by half the row's number, so that the 16 lanes that are served
 // together (16 rows, one chunk) meet all 64 banks.
 // The direct loads are asm: as a builtin every LDS read behind them waits for all of them.
-__device__ __forceinline__ void request16(const void* uniform_src, unsigned lane_bytes, unsigned lds_dst)
-{
-    int m0;                                                              // given back: the compiler does not let an asm statement change it
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-                 : "=&s"(m0) : "s"(lds_dst), "v"(lane_bytes), "s"(uniform_src) : "memory");
-}
-__device__ __forceinline__ void request4(const void* uniform_src, unsigned lane_bytes, unsigned lds_dst)
-{
-    int m0;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b32 m0, %0"
-                 : "=&s"(m0) : "s"(lds_dst), "v"(lane_bytes), "s"(uniform_src) : "memory");
-}
+// Nothing for stages from `end` on, which the asm finds out: a branch around it would be one in the middle of a stage.
+#define MIXAQ_REQUEST(SIZE_)                                                                                                              \
+    int m0; /* given back: the compiler does not let an asm statement change it */                                                       \
+    asm volatile("s_cmp_ge_i32 %4, %5\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_" SIZE_ \
+                 " %2, %3\n\ts_mov_b32 m0, %0\n.Lskip%=:" : "=&s"(m0) : "s"(lds_dst), "v"(lane_bytes), "s"(uniform_src), "s"(stage), "s"(end) : "memory", "scc")
+__device__ __forceinline__ void request16(const void* uniform_src, unsigned lane_bytes, unsigned lds_dst, int stage, int end) { MIXAQ_REQUEST("dwordx4"); }
+__device__ __forceinline__ void request4(const void* uniform_src, unsigned lane_bytes, unsigned lds_dst, int stage, int end) { MIXAQ_REQUEST("dword"); }
+#undef MIXAQ_REQUEST
 __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)p; }
 
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -399,18 +407,40 @@ __device__ __forceinline__ v16f half_product(const v4i (&w)[4], const v4i (&x)[4
     }
 }
 
+// Of instructions of 32 x 32 the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, and lane half h takes the 16-byte chunks h, 2 + h, 4 + h
+// and 6 + h of a row's 128 bytes.  Result e is row 8 (e / 4) + 4 h + e % 4: of the outputs, by output_of, number 4 (2 (T % 2) + e / 8) + e % 4 of
+// run 2 (e / 4 % 2) + h of 16, in half T / 2 of the block.
+__device__ __forceinline__ int run_of(int i, int h) { return (i >> 1) * 64 + (2 * (i & 1) + h) * 16; }
+__device__ __forceinline__ void in_runs(const v16f (&acc)[4], float (&v)[64])
+{
+#pragma unroll
+    for (int T = 0; T < 4; ++T)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[((T >> 1) * 2 + (e >> 2 & 1)) * 16 + ((T & 1) * 2 + (e >> 3)) * 4 + (e & 3)] = acc[T][e];
+}
+__device__ __forceinline__ void bias_of(const float* bias, int T, int h, v16f& acc)      // of the block's 128, for the results of the T-th
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        v4f b;
+        __builtin_memcpy(&b, bias + run_of((T >> 1) * 2 + (q & 1), h) + ((T & 1) * 2 + (q >> 1)) * 4, 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[q * 4 + e] = b[e];
+    }
+}
+
 constexpr int MOST_KB = 65536 / SBLOCK;
-constexpr int GROUP_M = 8;                        // row tiles that run beside one another
+constexpr int GROUP_M = 4;                        // row tiles that run beside one another
 
 template <int YT, int MT, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int tiles_m, int tiles_n, FastDiv by_group)
+__global__ __launch_bounds__(WM * WN * 64, 2) void tile_kernel(LinearArgs A, int tiles_m, int tiles_n, FastDiv by_group)
 {
     constexpr bool EXACT = exact_sums(YT);
     constexpr int W = WM * WN, TM = 32 * MT * WM;
     constexpr int XP = TM * 8 / 64, WP = WN * 16, XL = XP / W, WL = WP / W;  // 1 KB pieces of a stage, of x and of w, and a wave's
     static_assert(XP % W == 0 && WP % W == 0 && TM / 64 <= W, "whole pieces a wave");
     __shared__ v4i xs[2][XP * 64], ws[2][WP * 64];
-    __shared__ float sxs[2][TM], sws[WN][MOST_KB];
+    __shared__ float sxs[2][TM], sws[WN][MOST_KB + 1];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
     const int wm = wave / WN, wn = wave % WN;
     // a run of tiles per XCD, in groups of GROUP_M row tiles with all their outputs, so that what its CUs read at one time meets in its L2
@@ -438,10 +468,10 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
     auto request_x = [&](int kb, int i) {
         unsigned o = at[i];
         if (kb >= kb_tail && kb * SBLOCK + chunk[i & 1] >= A.K) o -= chunk[i & 1];
-        request16(xb + kb * SBLOCK, o, lx + ((kb & 1) * XP + wave * XL + i) * 1024);
+        request16(xb + kb * SBLOCK, o, lx + ((kb & 1) * XP + wave * XL + i) * 1024, kb, KB);
     };
-    auto request_w = [&](int kb, int i) { request16(wb + (long long)kb * (8 * TILE_BYTES) + i * 1024, lane * 16, lw + ((kb & 1) * WP + wave * WL + i) * 1024); };
-    auto request_s = [&](int kb) { request4(sxb + kb * A.ldsx, srow, ls + ((kb & 1) * TM + swave * 64) * 4); };
+    auto request_w = [&](int kb, int i) { request16(wb + (long long)kb * (8 * TILE_BYTES) + i * 1024, lane * 16, lw + ((kb & 1) * WP + wave * WL + i) * 1024, kb, KB); };
+    auto request_s = [&](int kb) { request4(sxb + kb * A.ldsx, srow, ls + ((kb & 1) * TM + swave * 64) * 4, kb, KB); };
     auto landed = [&] {                                                      // every wave's requests, and its reads of the other buffer have returned
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -457,30 +487,15 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
         sws[n][kb] = A.sw[kb * A.NB + min(nb0 + n, A.NB - 1)];
     }
     const int m0 = wm * 32 * MT;
+    static_assert(2 * XP * 64 >= W * 512, "room for a wave's 32 rows of 256 bytes");
+    v4i* const turn = &xs[0][0] + wave * 512;                                // (at the end)
     auto scale_of = [&](int kb, int row) { return sxs[kb & 1][row] * sws[wn][kb]; };
-    // `left`: of the row's bytes from a chunk on; what stands behind them takes no part
-    auto cut = [&](v4i& c, int left) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) c[q] &= left >= 4 * q + 4 ? -1 : left <= 4 * q ? 0 : (1 << (8 * (left - 4 * q))) - 1;
-    };
-    auto all_stages = [&](auto&& stage, auto&& cut_rows) {
-        constexpr std::true_type yes;
-        constexpr std::false_type no;
-        int kb = 0;
-#pragma unroll 1
-        for (; kb < KB - 2; ++kb) stage(kb, yes, yes);
-        if (KB > 1) stage(kb++, yes, no);
-        if (A.K & 15) cut_rows(A.K - kb * SBLOCK);
-        stage(kb, no, no);
-    };
     landed();
-    if (KB > 1) {
 #pragma unroll
-        for (int i = 0; i < XL; ++i) request_x(1, i);
+    for (int i = 0; i < XL; ++i) request_x(1, i);
 #pragma unroll
-        for (int i = 0; i < WL; ++i) request_w(1, i);
-        request_s(1);
-    }
+    for (int i = 0; i < WL; ++i) request_w(1, i);
+    request_s(1);
     // The stages.  Beside a product run the sums of an earlier one, whose result is there by then: matrix and vector work of a wave side by side.  What
     // a product needs of LDS is read some products ahead; behind the last read of a stage the waves meet, and its buffer is requested anew.
     // (Without branches in a stage: the compiler moves the sums behind any, away from the matrix instructions.)
@@ -489,7 +504,13 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
         constexpr int MI = 2 * MT, P = 8 * MI, BEHIND = 2;
         static_assert(MI >= BEHIND, "the products of a stage that are added in the next one");
         const int c = lane & 15, g = lane >> 4;
-        v4f acc[MI][8] = {}, d[4] = {};
+        v4f acc[MI][8], d[4] = {};
+#pragma unroll
+        for (int T = 0; T < 8; ++T) {
+            __builtin_memcpy(&acc[0][T], A.bias + min(nb, A.NB - 1) * SBLOCK + output_of(T, 4 * g), 16);
+#pragma unroll
+            for (int i = 1; i < MI; ++i) acc[i][T] = acc[0][T];
+        }
         v4i x[MI][2], w[3][2];
         float s[MI], s_last[BEHIND] = {};
         const v4i* const xr[2] = {&xs[0][(m0 + c) * 8 + (g ^ (c >> 1))], &xs[0][(m0 + c) * 8 + ((g + 4) ^ (c >> 1))]};
@@ -513,7 +534,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
             read_x(0, i);
             s[i] = scale_of(0, m0 + i * 16 + c);
         }
-        all_stages([&](int kb, auto more, auto request) {
+        auto stage = [&](int kb, auto more) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const int T = p / MI, i = p % MI, behind = (p + P - BEHIND) % P;
@@ -525,7 +546,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
                 __builtin_amdgcn_sched_barrier(0);
                 add(behind, p < BEHIND ? s_last[p] : s[behind % MI]);
                 if (T == 7 && more) read_x(kb + 1, i);
-                if (T >= 6 && request) {                                     // a request a product
+                if (T >= 6 && more) {                                     // a request a product
                     const int q = p - 6 * MI, per = (XL + WL + 2 * MI - 1) / (2 * MI);
 #pragma unroll
                     for (int k = q * per; k < (q + 1) * per; ++k) {
@@ -536,24 +557,38 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (more) {
-                // w of the next stage's first tiles lie where (8 + T) % 3 says: back to their places
-                const v4i a0 = w[2][0], a1 = w[2][1], b0 = w[0][0], b1 = w[0][1];
-                w[0][0] = a0; w[0][1] = a1; w[1][0] = b0; w[1][1] = b1;
+            // w of the next stage's first tiles lie where (8 + T) % 3 says: back to their places
+            const v4i a0 = w[2][0], a1 = w[2][1], b0 = w[0][0], b1 = w[0][1];
+            w[0][0] = a0; w[0][1] = a1; w[1][0] = b0; w[1][1] = b1;
 #pragma unroll
-                for (int b = 0; b < BEHIND; ++b) s_last[b] = s[MI - BEHIND + b];
+            for (int b = 0; b < BEHIND; ++b) s_last[b] = s[MI - BEHIND + b];
 #pragma unroll
-                for (int i = 0; i < MI; ++i) s[i] = scale_of(kb + 1, m0 + i * 16 + c);
-            }
-        }, [&](int left) {
+            for (int i = 0; i < MI; ++i)
+                if (more) s[i] = scale_of(kb + 1, m0 + i * 16 + c);
+        };
+        auto cut_rows = [&] {                                                // what stands behind a row's end takes no part
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                cut(x[i][0], left - g * 16);
-                cut(x[i][1], left - g * 16 - 64);
+                cut(x[i][0], A.K - (KB - 1) * SBLOCK - g * 16);
+                cut(x[i][1], A.K - (KB - 1) * SBLOCK - g * 16 - 64);
             }
-        });
+        };
+        // Of the large tile the stage stands here once, and the last one reads on like the others, for nobody: with a copy of its own some sums
+        // would lie in scratch memory at the end, and a launch with scratch costs the more (16384 x 1024 x 4096 113 -> 84 us).  Small tiles
+        // of few stages are faster with it (268324 x 128 x 512 of bf16 97 -> 88).
+        constexpr bool ONCE = MT > 1;
+#pragma unroll 1
+        for (int kb = 0; kb < (ONCE ? KB : KB - 1); ++kb) {
+            if (ONCE && kb == KB - 1 && (A.K & 15)) cut_rows();
+            stage(kb, std::true_type());
+        }
+        if constexpr (!ONCE) {
+            if (A.K & 15) cut_rows();
+            stage(KB - 1, std::false_type());
+        }
 #pragma unroll
-        for (int b = 0; b < BEHIND; ++b) add(P - BEHIND + b, s[MI - BEHIND + b]);
+        for (int b = 0; b < BEHIND; ++b) add(P - BEHIND + b, s_last[b]);
+        __syncthreads();                                                     // the last stage has been read
         if (nb >= A.NB) return;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -562,13 +597,18 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
             for (int T = 0; T < 8; ++T)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[T * 4 + e] = acc[i][T][e];
-            finish<YT, 2, 16>(A, v, nb, row0 + m0 + i * 16 + c, [&](int r) { return r * 64 + g * 16; });
+            finish<YT, 2, 16>(A, v, nb, row0 + m0 + i * 16, turn, [&](int r) { return r * 64 + g * 16; });
         }
     } else {
-        // instructions of 32 x 32 x 16 (those of 16 x 16 have half their rate): the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, lane
-        // half h takes the chunks h, 2 + h, 4 + h and 6 + h of a row
+        // instructions of 32 x 32 x 16: those of 16 x 16 have half their rate
         constexpr int P = 4 * MT;
-        v16f acc[MT][4] = {}, d[2] = {};
+        v16f acc[MT][4], d[2] = {};
+#pragma unroll
+        for (int T = 0; T < 4; ++T) {
+            bias_of(A.bias + min(nb, A.NB - 1) * SBLOCK, T, h, acc[0][T]);
+#pragma unroll
+            for (int m = 1; m < MT; ++m) acc[m][T] = acc[0][T];
+        }
         v4i x[MT][4], w[2][4];
         float s[MT], s_last = 0.0f;                                          // of this stage's rows; of the product still to be added
         auto read_x = [&](int kb, int m) {
@@ -590,7 +630,7 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
             read_x(0, m);
             s[m] = scale_of(0, m0 + m * 32 + j);
         }
-        all_stages([&](int kb, auto more, auto request) {
+        auto stage = [&](int kb, auto more) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const int T = p / MT, m = p % MT, last = (p + P - 1) % P;
@@ -607,38 +647,36 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void tile_kernel(LinearArgs A, int
                 d[p & 1] = half_product<EXACT, 1>(w[T & 1], x[m], d[p & 1]);
                 add(last, d[(p & 1) ^ 1], scale, 1);
                 __builtin_amdgcn_sched_barrier(0);
+                if (T == 3 && m == MT - 1) s_last = s[m];
                 if (T == 3 && more) {
-                    if (m == MT - 1) s_last = s[m];
                     read_x(kb + 1, m);
                     s[m] = scale_of(kb + 1, m0 + m * 32 + j);
-                    if (request) {
 #pragma unroll
-                        for (int i = m * XL / MT; i < (m + 1) * XL / MT; ++i) request_x(kb + 2, i);
+                    for (int i = m * XL / MT; i < (m + 1) * XL / MT; ++i) request_x(kb + 2, i);
 #pragma unroll
-                        for (int i = m * WL / MT; i < (m + 1) * WL / MT; ++i) request_w(kb + 2, i);
-                        if (m == 0) request_s(kb + 2);
-                    }
+                    for (int i = m * WL / MT; i < (m + 1) * WL / MT; ++i) request_w(kb + 2, i);
+                    if (m == 0) request_s(kb + 2);
                 }
             }
-        }, [&](int left) {
+        };
+#pragma unroll 1
+        for (int kb = 0; kb < KB - 1; ++kb) stage(kb, std::true_type());
+        if (A.K & 15) {                                                      // what stands behind a row's end takes no part
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) cut(x[m][c], left - (2 * c + h) * 16);
-        });
-        add(P - 1, d[(P - 1) & 1], s[MT - 1], 0);
-        add(P - 1, d[(P - 1) & 1], s[MT - 1], 1);
+                for (int c = 0; c < 4; ++c) cut(x[m][c], A.K - (KB - 1) * SBLOCK - (2 * c + h) * 16);
+        }
+        stage(KB - 1, std::false_type());
+        add(P - 1, d[(P - 1) & 1], s_last, 0);
+        add(P - 1, d[(P - 1) & 1], s_last, 1);
+        __syncthreads();                                                     // the last stage has been read
         if (nb >= A.NB) return;
-        // result e of the T-th instruction is its row 8 (e / 4) + 4 h + e % 4: of the outputs, with output_of, number 4 (2 (T % 2) + e / 8) + e % 4 of
-        // run 2 (e / 4 % 2) + h of 16, in half T / 2 of the block
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             float v[64];
-#pragma unroll
-            for (int T = 0; T < 4; ++T)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[((T >> 1) * 2 + (e >> 2 & 1)) * 16 + ((T & 1) * 2 + (e >> 3)) * 4 + (e & 3)] = acc[m][T][e];
-            finish<YT, 4, 32>(A, v, nb, row0 + m0 + m * 32 + j, [&](int i) { return (i >> 1) * 64 + (2 * (i & 1) + h) * 16; });
+            in_runs(acc[m], v);
+            finish<YT, 4, 32>(A, v, nb, row0 + m0 + m * 32, turn, [&](int i) { return run_of(i, h); });
         }
     }
 }
