@@ -704,15 +704,25 @@ int launch_split(const LinearArgs& A, hipStream_t st)
     return MIXAQ_OK;
 }
 
-// Which kernel takes a product: by rows, K and N alone, so that the sums are the same whatever the types of x and y.
+// Which kernel takes a product: by rows, K, N and how sums are taken, never by x's type or by whether exact sums become codes, so that values
+// in and codes out are the same results.  us (graph replays; few / split / tile / large):
+//   FEW while its workgroups - 16 rows and 16 outputs each - times their blocks of K stay few, and for up to 16 rows:
+//     64 x 1024 x 1024 3.2 / 7.1    128 x 4096 x 1024 7.3 / 16.8    256 x 1024 x 1024 4.9 / 7.2    1001 x 1000 x 333 5.8 / 7.2    64 x 4096 x 4096
+//     11.8 / 16.9 |  1024 x 1024 x 1024 13.2 / 8.0    512 x 2048 x 2048 22.9 / 11.5    256 x 4096 x 4096 39.5 / 19.1
+//   SPLIT below 96 tiles of 128 x 128, codes out: 1024 x 1024 x 1024 8.9 / 10.9 (tile)    1024 x 4096 x 1024 21.4 / 39.3 |  4704 x 1536 x 384 (111 tiles)
+//     21.8 / 17.6    8192 x 256 x 256 (128) 10.6 / 5.7; bf16 out the same or 5 % to either side at 64
+//   LARGE, 16-bit sums, from 192 tiles of 256 x 256 and two blocks of K: 16384 x 512 x 512 (128) 11.3 (tile) / 13.9    2048 x 1024 x 4096 (128)
+//     15.4 / 19.0 |  16384 x 768 x 768 (192) 18.7 / 17.4    8192 x 256 x 2048 (256) 14.2 / 12.8    4096 x 2048 x 4096 (256) 43.9 / 34.9
+//   LARGE, exact sums, from 224 tiles of 256 x 128 and three blocks: 4096 x 4096 x 1024 (128) 42.6 (tile) / 50.9    65536 x 256 x 1024 (two blocks)
+//     56.1 / 60.8 |  4704 x 384 x 1536 (228) 10.8 / 10.4    8192 x 1024 x 1024 (256) 22.4 / 19.7    16384 x 1024 x 2048 75.3 / 70.2
 enum Form { FORM_FEW, FORM_SPLIT, FORM_TILE, FORM_LARGE };
-Form form_of(int M, const mixaq_scaled_linear* h, long long ldx)
+Form form_of(int M, const mixaq_scaled_linear* h, bool exact, long long ldx)
 {
-    const long long tiles128 = (M + 127LL) / 128 * h->NB, tiles256 = (M + 255LL) / 256 * ((h->NB + 1) / 2);
-    if (M <= 64) return FORM_FEW;
-    if (ldx >= (1 << 22)) return FORM_SPLIT;
-    if (tiles256 >= 256 && h->KB >= 4) return FORM_LARGE;
-    return tiles128 >= 256 ? FORM_TILE : FORM_SPLIT;
+    const long long tiles16 = (M + 15LL) / 16 * h->NB * 8, tiles128 = (M + 127LL) / 128 * h->NB;
+    const long long large = (M + 255LL) / 256 * (exact ? h->NB : (h->NB + 1) / 2);
+    if (M <= 16 || tiles16 * h->KB <= 5000 + 1400LL * h->KB) return FORM_FEW;
+    if (tiles128 < 96 || ldx >= (1 << 22)) return FORM_SPLIT;                 // (rows 4 MB apart: the tiles count in 32 bits)
+    return large >= (exact ? 224 : 192) && h->KB >= (exact ? 3 : 2) ? FORM_LARGE : FORM_TILE;
 }
 
 template <int XT, int YT>
@@ -746,7 +756,7 @@ size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 // the workspace: codes and scales of x, where it is given as values and not quantized on its way into the product
 size_t workspace_of(const mixaq_scaled_linear* h, int32_t rows, int32_t x_type)
 {
-    if (x_type == MIXAQ_E4M3 || rows == 0 || form_of(rows, h, 0) == FORM_FEW) return 0;
+    if (x_type == MIXAQ_E4M3 || rows == 0 || form_of(rows, h, true, 0) == FORM_FEW) return 0;      // (FEW whatever the sums)
     return align256((size_t)rows * round_up16(h->d.K)) + align256((size_t)rows * h->KB * 4);
 }
 
@@ -851,7 +861,7 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
     A.sy = y->scales; A.ldsy = y->scale_stride;
     A.M = rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
     A.gelu = h->d.activation == 1;
-    const Form form = form_of(rows, h, A.ldx);
+    const Form form = form_of(rows, h, exact_sums(y->type), A.ldx);
     int x_type = x->type;
     if (need) {
         rc = launch_quantize(*x, rows, K, 1, codes, st);

@@ -39,22 +39,14 @@ def blocks(n):
 def quantize(x, block_rows=1):
     """x: binary32 values [rows, cols] -> codes uint8 [rows, cols], scales [ceil(cols / 128), ceil(rows / block_rows)]."""
     rows, cols = x.shape
-    x = x.astype(np.float64)
-    codes, scales = np.zeros((rows, cols), np.uint8), np.zeros((blocks(cols), -(-rows // block_rows)))
-    for i in range(scales.shape[1]):
-        for b in range(scales.shape[0]):
-            part = x[i * block_rows:(i + 1) * block_rows, b * 128:(b + 1) * 128]
-            top = np.max(np.abs(part))
-            if not np.isfinite(top):
-                scale, inv = np.nan, np.nan
-            else:
-                scale = f32(max(top, 2.0 ** -100) / 448.0)
-                inv = f32(1.0 / scale)
-            scales[b, i] = scale
-            with np.errstate(invalid="ignore"):
-                q = np.clip(f32(part * inv), -448.0, 448.0)
-            codes[i * block_rows:(i + 1) * block_rows, b * 128:(b + 1) * 128] = nearest_code(np.full_like(q, np.nan) if np.isnan(scale) else q)
-    return codes, scales
+    v = np.pad(x.astype(np.float64), ((0, -rows % block_rows), (0, -cols % 128)))
+    v = v.reshape(v.shape[0] // block_rows, block_rows, -1, 128)
+    with np.errstate(invalid="ignore"):
+        top = np.abs(v).max((1, 3))
+        scale = np.where(np.isfinite(top), f32(np.maximum(top, 2.0 ** -100) / 448.0), np.nan)
+        q = np.clip(f32(v * f32(1.0 / scale)[:, None, :, None]), -448.0, 448.0)
+    codes = nearest_code(q).reshape(v.shape[0] * block_rows, -1)[:rows, :cols]
+    return np.ascontiguousarray(codes), np.ascontiguousarray(scale.T)
 
 
 def dequantize(codes, scales, block_rows=1):

@@ -160,7 +160,8 @@ def check_result(y, want, bound, kind):
 SIZES = [  # rows, K, N: one of everything, ends inside tiles, blocks and 16-byte chunks, each kernel's range and both sides of it
     (1, 1, 1), (1, 128, 128), (1, 1024, 512), (2, 96, 96), (3, 130, 40), (15, 1000, 333), (16, 384, 1536), (17, 257, 129), (31, 2048, 64),
     (33, 512, 200), (49, 768, 1000), (64, 129, 257), (65, 640, 72), (100, 4096, 136), (128, 128, 512), (129, 1536, 384), (200, 31, 1000),
-    (257, 256, 256), (513, 1024, 1024), (1001, 1000, 333), (1024, 512, 2048), (2400, 384, 1536), (4704, 96, 384), (3000, 128, 512)]
+    (257, 256, 256), (513, 1024, 1024), (1001, 1000, 333), (1024, 512, 2048), (2400, 384, 1536), (4704, 96, 384), (3000, 128, 512),
+    (700, 1500, 700), (3001, 200, 600), (6200, 300, 2000), (12300, 520, 1000)]
 
 
 @pytest.mark.parametrize("x_kind,y_kind", [("e4m3", "bf16"), ("e4m3", "e4m3"), ("e4m3", "f32"), ("bf16", "f16"), ("f32", "f32"), ("f16", "e4m3")])
@@ -180,7 +181,7 @@ def test_layer(rows, K, N, x_kind, y_kind):
         assert y.untouched()
 
 
-@pytest.mark.parametrize("rows,K,N", [(1, 1024, 512), (40, 384, 200), (70, 200, 384), (300, 512, 300), (2000, 256, 640)])
+@pytest.mark.parametrize("rows,K,N", [(1, 1024, 512), (40, 384, 200), (70, 200, 384), (300, 512, 300), (2000, 256, 640), (3001, 200, 600), (6200, 300, 2000)])
 @pytest.mark.parametrize("activation", ["none", "gelu"])
 def test_values_and_codes_are_two_forms_of_one_call(rows, K, N, activation):
     """Values in: the result of quantizing them first.  Codes out: the 32-bit result quantized."""
@@ -202,23 +203,23 @@ def test_values_and_codes_are_two_forms_of_one_call(rows, K, N, activation):
         assert torch.equal(half[0].t, half[1].t)
 
 
-@pytest.mark.parametrize("rows", [3, 50, 300, 1500])
+@pytest.mark.parametrize("rows", [3, 50, 300, 4000, 20000, 30000, 50000])
 def test_a_row_depends_on_nothing_but_itself(rows):
     """A NaN, an infinity or a huge row changes no other row, and the bytes behind a row's columns change nothing."""
     K, N = 300, 200
     with Layer(21, N, K) as layer:
         v = values(22, rows, K)
         x, _ = quantized(v)
-        a = Room(rows, N, "f32")
-        layer.run(x, a)
         v[1, 299], v[2, 0] = float("nan"), float("inf")
         z, _ = quantized(v)
         z.buffer[:, K:] = 0x7F                                  # NaN codes
-        b = Room(rows, N, "f32")
-        layer.run(z, b)
-        assert torch.isnan(b.t[1:3]).all()
         keep = [r for r in range(rows) if r not in (1, 2)]
-        assert torch.equal(a.t[keep], b.t[keep])
+        for kind in ("f32", "bf16"):                            # both kinds of sums
+            a, b = Room(rows, N, kind), Room(rows, N, kind)
+            layer.run(x, a)
+            layer.run(z, b)
+            assert torch.isnan(b.t[1:3]).all()
+            assert torch.equal(a.t[keep], b.t[keep])
         c = Room(rows, N, "e4m3")
         layer.run(z, c)
         assert torch.isnan(c.scales[:, 1:3]).all() and (bytes_of(c.t)[1:3] & 0x7F == 0x7F).all() and not torch.isnan(c.scales[:, keep]).any()
@@ -253,8 +254,9 @@ def test_gelu_far_from_zero():
 
 def test_layer_refuses():
     with Layer(3, 100, 200) as layer:
-        x, y = placed(values(1, 80, 200), "bf16"), Room(80, 100, "f32")
-        ws = M.alloc_linear_workspace(layer.h, 80, torch.bfloat16, torch.float32)
+        n = 10000                                               # (few rows need no workspace)
+        x, y = placed(values(1, n, 200), "bf16"), Room(n, 100, "f32")
+        ws = M.alloc_linear_workspace(layer.h, n, torch.bfloat16, torch.float32)
         assert ws.numel() and M.mixaq_scaled_linear_workspace_bytes(layer.h, 8, torch.bfloat16, torch.float32) == 0
         call = M.mixaq_scaled_linear_forward
 
@@ -267,16 +269,16 @@ def test_layer_refuses():
         refused(-4, "needed", x.t, y.t, workspace=ws[:-1])
         refused(-4, "aligned", x.t, y.t, workspace=torch.empty(ws.numel() + 256, dtype=torch.uint8, device="cuda")[16:])
         refused(-2, "overlap", x.t, x.t[:, :100], workspace=ws)
-        large = torch.zeros(65536, dtype=torch.uint8, device="cuda")
-        refused(-2, "workspace overlaps", large.view(torch.bfloat16)[:16000].view(80, 200), y.t, workspace=large)
+        large = torch.zeros(n * 512, dtype=torch.uint8, device="cuda")
+        refused(-2, "workspace overlaps", large.view(torch.bfloat16)[:n * 200].view(n, 200), y.t, workspace=large)
         with pytest.raises(ValueError, match="do not fit"):
             call(layer.h, x.t[:, :199], y.t, workspace=ws)
         with pytest.raises(ValueError, match="scales"):
-            call(layer.h, Room(80, 200, "e4m3").t, y.t, workspace=ws)
+            call(layer.h, Room(n, 200, "e4m3").t, y.t, workspace=ws)
         with pytest.raises(ValueError, match="scales"):
-            call(layer.h, x.t, y.t, x_scales=torch.ones((2, 80), device="cuda"), workspace=ws)
+            call(layer.h, x.t, y.t, x_scales=torch.ones((2, n), device="cuda"), workspace=ws)
         call(layer.h, x.t[:0], y.t[:0])                         # nothing to do
-        wide = torch.zeros((80, 512), dtype=torch.bfloat16, device="cuda")
+        wide = torch.zeros((n, 512), dtype=torch.bfloat16, device="cuda")
         call(layer.h, wide[:, :200], wide[:, 200:300], workspace=ws)     # columns of one matrix are no overlap
 
 
@@ -436,9 +438,9 @@ def test_feed_forward(rows, C, hidden, kind):
     ffn.close()
 
 
-def test_feed_forward_captured_and_on_streams():
+@pytest.mark.parametrize("rows,C,hidden", [(130, 384, 800), (3000, 256, 1024)])
+def test_feed_forward_captured_and_on_streams(rows, C, hidden):
     """A captured run, replayed on new inputs among eager runs of another instance on other streams, gives the eager bits every time."""
-    rows, C, hidden = 130, 384, 800
     a, b = FeedForward(rows, C, hidden, "bf16"), FeedForward(rows, C, hidden, "bf16")
     xs = [values(40 + i, rows, C).bfloat16().cuda() for i in range(4)]
     x = xs[0].clone()
@@ -467,7 +469,7 @@ def test_feed_forward_captured_and_on_streams():
 def test_one_layer_on_two_streams_at_once():
     """The handle is shared, the workspaces are not; every repetition gives the same bits."""
     with Layer(50, 640, 512, activation="gelu") as layer:
-        x = [placed(values(60 + i, 200 + 800 * i, 512), "bf16") for i in range(2)]
+        x = [placed(values(60 + i, 2500 + 800 * i, 512), "bf16") for i in range(2)]
         want = [Room(v.t.shape[0], 640, "bf16") for v in x]
         for v, w in zip(x, want):
             layer.run(v, w)
@@ -485,10 +487,11 @@ def test_one_layer_on_two_streams_at_once():
 
 def test_larger_workspace_than_needed_and_growing_rows():
     with Layer(70, 300, 200) as layer:
-        sizes = [M.mixaq_scaled_linear_workspace_bytes(layer.h, r, torch.float32, torch.float8_e4m3fn) for r in (0, 1, 5, 64, 65, 1000, 5000)]
+        sizes = [M.mixaq_scaled_linear_workspace_bytes(layer.h, r, torch.float32, torch.float8_e4m3fn) for r in (0, 1, 5, 64, 65, 1000, 4000, 5000)]
         assert sizes == sorted(sizes)
         ws = torch.empty(sizes[-1], dtype=torch.uint8, device="cuda")
-        for rows in (1, 5, 64, 65, 1000):                        # what serves the most rows serves fewer
+        assert sizes[-1] > 0
+        for rows in (1, 5, 64, 65, 1000, 4000, 5000):            # what serves the most rows serves fewer
             x, y = placed(values(rows, rows, 200), "f32"), Room(rows, 300, "f32")
             M.mixaq_scaled_linear_forward(layer.h, x.t, y.t, workspace=ws)
             x64 = R.dequantize(*R.quantize(as64(x.t).astype(np.float32)))
