@@ -453,8 +453,10 @@ def mixaq_scaled_linear_forward(h, x, y, x_scales=None, y_scales=None, workspace
 class ResidualNorm:
     """What mixaq_residual_norm takes besides the rows; keeps its vectors alive."""
 
-    def __init__(self, desc, params, vectors, gates):
-        self.desc, self.params, self.vectors, self.gates = desc, params, vectors, gates
+    def __init__(self, desc, params, vectors, most_rows):
+        self.desc, self.params, self.vectors = desc, params, vectors
+        self.channels, self.most_rows = desc.C, most_rows             # most_rows: that the gate's vectors are enough for
+        self.args = C.byref(desc), C.byref(params)
 
 
 def make_residual_norm(channels, post="none", pre="layer", eps=1e-5, residual_scale=1.0, post_gamma=None, post_beta=None, pre_gamma=None,
@@ -470,19 +472,19 @@ def make_residual_norm(channels, post="none", pre="layer", eps=1e-5, residual_sc
                                                        (pre_beta, "pre_beta"))] + [gate]
     span = 2**31 - 1 if rows_per_gate is None else int(rows_per_gate)
     desc = ResidualNormDesc(channels, NORMS[post], NORMS[pre], span, eps, eps, residual_scale)
-    return ResidualNorm(desc, ResidualNormParams(*[_ptr(v) for v in vectors]), vectors, None if gate is None else gate.shape[0])
+    return ResidualNorm(desc, ResidualNormParams(*[_ptr(v) for v in vectors]), vectors, 2**31 - 1 if gate is None else gate.shape[0] * span)
 
 
 def mixaq_residual_norm(norm, x, branch=None, y=None, out=None, out_scales=None, stream=None):
     """y = residual_scale * x + gate * post(branch), out = pre(y); all [rows, C], y or out may be None (not stored)."""
-    rows = x.shape[0]
-    for t, n in ((x, "x"), (branch, "branch"), (y, "y"), (out, "out")):
-        if t is not None and t.shape != (rows, norm.desc.C):
-            raise ValueError("%s has the shape %s, not (%d, %d)" % (n, tuple(t.shape), rows, norm.desc.C))
-    if norm.gates is not None and rows > norm.gates * norm.desc.rows_per_gate:
-        raise ValueError("%d rows need more than the %d gate vectors of %d rows each" % (rows, norm.gates, norm.desc.rows_per_gate))
-    _check(load().mixaq_residual_norm(C.byref(norm.desc), C.byref(norm.params), _rows(x, "x"), _rows(branch, "branch"), _rows(y, "y"),
-                                      _rows(out, "out", out_scales), rows, _stream(stream)))
+    shape = rows, _ = x.shape[0], norm.channels
+    if x.shape != shape or (branch is not None and branch.shape != shape) or (y is not None and y.shape != shape) or (out is not None and out.shape != shape):
+        raise ValueError("x, branch, y and out must be of shape %s (got %s)" % (shape, [None if t is None else tuple(t.shape) for t in (x, branch, y, out)]))
+    if rows > norm.most_rows:
+        raise ValueError("%d rows, but the gate has vectors for %d" % (rows, norm.most_rows))
+    desc, params = norm.args
+    _check(load().mixaq_residual_norm(desc, params, _rows(x, "x"), _rows(branch, "branch"), _rows(y, "y"), _rows(out, "out", out_scales), rows,
+                                      _stream(stream)))
     return y, out
 
 
