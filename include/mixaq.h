@@ -276,7 +276,7 @@ int mixaq_downsample_forward_taps(const mixaq_downsample *h, const float *x, flo
  * shorter) row r's scale is scales[b * scale_stride + r], and the values that codes stand for are code * scale.  Values may
  * start at any multiple of their size and have any stride >= columns.  Codes and their stride are multiples of 16 bytes, and every row
  * (the last one too) has room for its columns rounded up to 16: those bytes are read, what they hold changes nothing, and they are never
- * written. */
+ * written.  Calls take 0 .. 2^30 rows; of no rows nothing is read, the pointers included. */
 typedef enum { MIXAQ_F32 = 0, MIXAQ_F16 = 1, MIXAQ_BF16 = 2, MIXAQ_E4M3 = 3 } mixaq_type;
 typedef struct {
     void    *data;
@@ -297,7 +297,8 @@ int mixaq_scaled_quantize(const mixaq_rows *x, int32_t rows, int32_t columns, in
  * multiply-add with the product of the two scales takes the sum to the others; one rounding to y's type at the end.  Sums are binary32; for
  * a y of 16 bits the sum of a block is that of the 8-bit matrix instruction, which keeps 14 bits of eight neighbouring products, counted
  * from the largest of them.  x may be given as values: they are quantized first, as mixaq_scaled_quantize with block_rows 1 does, with the same
- * result.  y may be codes: the binary32 results are quantized, as mixaq_scaled_quantize does. */
+ * result (but codes whose rows lie 4 MB or more apart may be summed in another order).  y may be codes: the binary32 results are
+ * quantized, as mixaq_scaled_quantize does. */
 typedef struct {
     int32_t K, N;             /* inputs and outputs per row: 1 .. 65536                           */
     int32_t activation;       /* 0: none, 1: GELU (erf form)                                      */
@@ -316,8 +317,8 @@ int mixaq_scaled_linear_destroy(mixaq_scaled_linear *h);
 /* Bytes of device workspace that mixaq_scaled_linear_forward needs for up to `rows` rows of these types (0: none, workspace may be
  * NULL); a workspace is 256-byte aligned.  Calls that may overlap in time need workspaces of their own, captured ones included. */
 int mixaq_scaled_linear_workspace_bytes(const mixaq_scaled_linear *h, int32_t rows, int32_t x_type, int32_t y_type, size_t *bytes);
-/* Allocates nothing and does not wait; may be captured.  x, y and workspace must not overlap.  rows may be 0.  The handle is not
- * changed: calls on any streams of its device may share it. */
+/* Allocates nothing and does not wait; may be captured.  The memory of x, y (scales included) and workspace must not overlap.  The handle
+ * is not changed: calls on any streams of its device, which has to be current, may share it. */
 int mixaq_scaled_linear_forward(const mixaq_scaled_linear *h, const mixaq_rows *x, int32_t rows, const mixaq_rows *y, void *workspace,
                                 size_t workspace_bytes, void *stream);
 
@@ -341,7 +342,7 @@ typedef struct {
 /* x: values.  branch: values, or NULL (y = residual_scale * x; then no post_norm and no gate).  y: values of x's type, or NULL.  out:
  * values, or codes as mixaq_scaled_quantize with block_rows 1 makes them of the binary32 results, or NULL (then no pre_norm); one
  * of y and out is given.  y or out may be x or branch itself (same data, stride and type); apart from that the outputs overlap
- * neither the inputs nor each other.  One kernel, allocates nothing.  rows may be 0. */
+ * neither the inputs nor each other.  One kernel, allocates nothing. */
 int mixaq_residual_norm(const mixaq_residual_norm_desc *desc, const mixaq_residual_norm_params *params, const mixaq_rows *x,
                         const mixaq_rows *branch, const mixaq_rows *y, const mixaq_rows *out, int32_t rows, void *stream);
 

@@ -388,6 +388,12 @@ def _rows(t, name, scales=None, block_rows=1):
     return Rows(t.data_ptr(), row, kind, scales.data_ptr(), scales.stride(0) if cols > 128 else across)
 
 
+def _choice(names, value, what):
+    if value not in names:
+        raise ValueError("%s must be one of %s (got %r)" % (what, ", ".join(names), value))
+    return names[value]
+
+
 def _on_device(t, name):
     at = t.get_device()
     if at < 0 or at != torch._C._cuda_getDevice():
@@ -419,7 +425,7 @@ def mixaq_scaled_linear_create(w, s_w, bias=None, activation="none", stream=None
     """w: float8_e4m3fn [N, K], s_w: float [ceil(K / 128), ceil(N / 128)] as of mixaq_scaled_quantize with block_rows 128; bias: float [N]
     or None; activation: "none" or "gelu".  Returns an opaque handle; w, s_w and bias may be released."""
     p = ScaledLinearParams(_rows(w, "w", s_w, 128), _ptr(_vector(bias, "bias", (w.shape[0],))))
-    d = ScaledLinearDesc(w.shape[1], w.shape[0], ACTIVATIONS[activation])
+    d = ScaledLinearDesc(w.shape[1], w.shape[0], _choice(ACTIVATIONS, activation, "activation"))
     out = C.c_void_p()
     _check(load().mixaq_scaled_linear_create(C.byref(d), C.byref(p), _stream(stream), C.byref(out)))
     out.K, out.N = w.shape[1], w.shape[0]
@@ -471,7 +477,7 @@ def make_residual_norm(channels, post="none", pre="layer", eps=1e-5, residual_sc
     vectors = [_vector(v, n, (channels,)) for v, n in ((post_gamma, "post_gamma"), (post_beta, "post_beta"), (pre_gamma, "pre_gamma"),
                                                        (pre_beta, "pre_beta"))] + [gate]
     span = 2**31 - 1 if rows_per_gate is None else int(rows_per_gate)
-    desc = ResidualNormDesc(channels, NORMS[post], NORMS[pre], span, eps, eps, residual_scale)
+    desc = ResidualNormDesc(channels, _choice(NORMS, post, "post"), _choice(NORMS, pre, "pre"), span, eps, eps, residual_scale)
     return ResidualNorm(desc, ResidualNormParams(*[_ptr(v) for v in vectors]), vectors, 2**31 - 1 if gate is None else gate.shape[0] * span)
 
 

@@ -243,7 +243,7 @@ extern "C" int mixaq_residual_norm(const mixaq_residual_norm_desc* desc, const m
     if (!params) return fail(MIXAQ_E_NULL, "params is NULL");
     const mixaq_residual_norm_desc& d = *desc;
     if (d.C < 1 || d.C > 16384) return fail(MIXAQ_E_SHAPE, "C=%d outside 1..16384", d.C);
-    if (rows < 0) return fail(MIXAQ_E_SHAPE, "rows must not be negative (got %d)", rows);
+    if (rows < 0 || rows > MOST_ROWS) return fail(MIXAQ_E_SHAPE, "need 0 <= rows <= 2^30 (got %d)", rows);
     int rc = check_norm(d.post_norm, d.post_eps, "post_norm");
     if (!rc) rc = check_norm(d.pre_norm, d.pre_eps, "pre_norm");
     if (rc) return rc;
@@ -262,12 +262,16 @@ extern "C" int mixaq_residual_norm(const mixaq_residual_norm_desc* desc, const m
     const char* names[2] = {"y", "out"};
     for (int i = 0; i < 2; ++i) {
         if (!outputs[i]) continue;
-        if (!same_place(*outputs[i], *x) && rows_overlap(*outputs[i], rows, d.C, *x, rows, d.C))
-            return fail(MIXAQ_E_SHAPE, "%s and x overlap", names[i]);
-        if (branch && !same_place(*outputs[i], *branch) && rows_overlap(*outputs[i], rows, d.C, *branch, rows, d.C))
-            return fail(MIXAQ_E_SHAPE, "%s and branch overlap", names[i]);
+        const Extent o = extent_of(*outputs[i], rows, d.C), os = scales_of(*outputs[i], rows, d.C);
+        for (const mixaq_rows* in : {x, branch}) {
+            if (!in) continue;
+            const Extent e = extent_of(*in, rows, d.C);
+            if ((!same_place(*outputs[i], *in) && overlap(o, e)) || overlap(os, e)) return fail(MIXAQ_E_SHAPE, "%s and %s overlap", names[i], in == x ? "x" : "branch");
+        }
+        if (overlap(o, os)) return fail(MIXAQ_E_SHAPE, "codes and scales of %s overlap", names[i]);
     }
-    if (y && out && rows_overlap(*y, rows, d.C, *out, rows, d.C)) return fail(MIXAQ_E_SHAPE, "y and out overlap");
+    if (y && out && (overlap(extent_of(*y, rows, d.C), extent_of(*out, rows, d.C)) || overlap(extent_of(*y, rows, d.C), scales_of(*out, rows, d.C))))
+        return fail(MIXAQ_E_SHAPE, "y and out overlap");
 
     NormArgs A = {};
     A.x = x->data; A.ldx = x->stride;

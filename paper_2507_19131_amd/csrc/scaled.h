@@ -147,8 +147,22 @@ inline int blocks_of(int columns) { return (columns + SBLOCK - 1) / SBLOCK; }
 
 // The matrix `m` as an argument called `name`: `columns` values or codes a row, scales for `scale_rows` rows.
 int check_rows(const mixaq_rows* m, const char* name, int32_t columns, bool codes_allowed, int32_t scale_rows);
-// Whether writing one matrix touches the other.  Column ranges of one larger matrix do not.
-bool rows_overlap(const mixaq_rows& a, int32_t rows_a, int32_t columns_a, const mixaq_rows& b, int32_t rows_b, int32_t columns_b);
+constexpr int32_t MOST_ROWS = 1 << 30;
+// Memory of an argument: `rows` runs of `width` bytes, `stride` apart.
+struct Extent {
+    uintptr_t at;
+    long long stride, rows, width;
+};
+inline Extent extent_of(const mixaq_rows& m, int32_t rows, int32_t columns)
+{
+    return {(uintptr_t)m.data, (long long)m.stride * size_of(m.type), rows, (long long)columns * size_of(m.type)};
+}
+inline Extent scales_of(const mixaq_rows& m, int32_t scale_rows, int32_t columns)        // (no rows where there are none)
+{
+    return {(uintptr_t)m.scales, (long long)m.scale_stride * 4, m.type == MIXAQ_E4M3 ? blocks_of(columns) : 0, (long long)scale_rows * 4};
+}
+// Whether writing one touches the other.  Column ranges of one larger matrix do not.
+bool overlap(const Extent& a, const Extent& b);
 // mixaq_scaled_quantize behind its checks
 int launch_quantize(const mixaq_rows& x, int32_t rows, int32_t columns, int32_t block_rows, const mixaq_rows& q, hipStream_t st);
 

@@ -821,7 +821,7 @@ int mixaq_scaled_linear_destroy(mixaq_scaled_linear* h)
 int mixaq_scaled_linear_workspace_bytes(const mixaq_scaled_linear* h, int32_t rows, int32_t x_type, int32_t y_type, size_t* bytes)
 {
     if (!h || !bytes) return fail(MIXAQ_E_NULL, "layer or bytes is NULL");
-    if (rows < 0) return fail(MIXAQ_E_SHAPE, "rows must not be negative (got %d)", rows);
+    if (rows < 0 || rows > MOST_ROWS) return fail(MIXAQ_E_SHAPE, "need 0 <= rows <= 2^30 (got %d)", rows);
     for (int t : {x_type, y_type})
         if (t < MIXAQ_F32 || t > MIXAQ_E4M3) return fail(MIXAQ_E_SHAPE, "unknown type %d", t);
     *bytes = workspace_of(h, rows, x_type);
@@ -832,13 +832,17 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
                                 size_t workspace_bytes, void* stream)
 {
     if (!h) return fail(MIXAQ_E_NULL, "layer is NULL");
-    if (rows < 0) return fail(MIXAQ_E_SHAPE, "rows must not be negative (got %d)", rows);
+    if (rows < 0 || rows > MOST_ROWS) return fail(MIXAQ_E_SHAPE, "need 0 <= rows <= 2^30 (got %d)", rows);
     if (rows == 0) return MIXAQ_OK;
     const int K = h->d.K, N = h->d.N;
     int rc = check_rows(x, "x", K, true, rows);
     if (!rc) rc = check_rows(y, "y", N, true, rows);
     if (rc) return rc;
-    if (rows_overlap(*x, rows, K, *y, rows, N)) return fail(MIXAQ_E_SHAPE, "x and y overlap");
+    const Extent in[2] = {extent_of(*x, rows, K), scales_of(*x, rows, K)}, out[2] = {extent_of(*y, rows, N), scales_of(*y, rows, N)};
+    for (const Extent& o : out)
+        for (const Extent& i : in)
+            if (overlap(o, i)) return fail(MIXAQ_E_SHAPE, "x and y overlap");
+    if (overlap(out[0], out[1])) return fail(MIXAQ_E_SHAPE, "codes and scales of y overlap");
     int device = -1;
     HIP_TRY(hipGetDevice(&device));
     if (device != h->device) return fail(MIXAQ_E_SHAPE, "the layer was created on device %d, device %d is current", h->device, device);
@@ -849,10 +853,8 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
         if (!workspace) return fail(MIXAQ_E_NULL, "workspace is NULL (%zu bytes needed)", need);
         if (workspace_bytes < need) return fail(MIXAQ_E_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
         if ((uintptr_t)workspace & 255) return fail(MIXAQ_E_WORKSPACE, "workspace must be 256-byte aligned");
-        const mixaq_rows ws = {workspace, (int64_t)need, MIXAQ_E4M3, nullptr, 0};
-        if (rows_overlap(ws, 1, (int32_t)std::min<size_t>(need, INT32_MAX), *x, rows, K) ||
-            rows_overlap(ws, 1, (int32_t)std::min<size_t>(need, INT32_MAX), *y, rows, N))
-            return fail(MIXAQ_E_SHAPE, "the workspace overlaps x or y");
+        const Extent ws = {(uintptr_t)workspace, 0, 1, (long long)need};
+        if (overlap(ws, in[0]) || overlap(ws, out[0]) || overlap(ws, out[1])) return fail(MIXAQ_E_SHAPE, "the workspace overlaps x or y");
         codes = {workspace, round_up16(K), MIXAQ_E4M3, (float*)((char*)workspace + align256((size_t)rows * round_up16(K))), rows};
     }
     LinearArgs A;

@@ -32,15 +32,14 @@ int check_rows(const mixaq_rows* m, const char* name, int32_t columns, bool code
     return MIXAQ_OK;
 }
 
-bool rows_overlap(const mixaq_rows& a, int32_t rows_a, int32_t columns_a, const mixaq_rows& b, int32_t rows_b, int32_t columns_b)
+bool overlap(const Extent& a, const Extent& b)
 {
-    const long long pa = (long long)(uintptr_t)a.data, pb = (long long)(uintptr_t)b.data;
-    const long long sa = a.stride * size_of(a.type), sb = b.stride * size_of(b.type);
-    const long long wa = (long long)columns_a * size_of(a.type), wb = (long long)columns_b * size_of(b.type);
-    if (pa + (rows_a - 1) * sa + wa <= pb || pb + (rows_b - 1) * sb + wb <= pa) return false;
-    if (sa == sb) {                                       // two column ranges of one matrix
-        const long long d = ((pb - pa) % sa + sa) % sa;   // b's first column behind a's
-        if (d >= wa && d + wb <= sa) return false;
+    if (!a.rows || !b.rows) return false;
+    const __int128 pa = a.at, pb = b.at;
+    if (pa + (__int128)(a.rows - 1) * a.stride + a.width <= pb || pb + (__int128)(b.rows - 1) * b.stride + b.width <= pa) return false;
+    if (a.stride == b.stride && a.stride > 0) {          // two column ranges of one matrix
+        const __int128 d = ((pb - pa) % a.stride + a.stride) % a.stride;           // b's first column behind a's
+        if (d >= a.width && d + b.width <= a.stride) return false;
     }
     return true;
 }
@@ -155,7 +154,7 @@ int launch_quantize(const mixaq_rows& x, int32_t rows, int32_t columns, int32_t 
 extern "C" int mixaq_scaled_quantize(const mixaq_rows* x, int32_t rows, int32_t columns, int32_t block_rows, const mixaq_rows* q,
                                      void* stream)
 {
-    if (rows < 0 || columns < 1) return fail(MIXAQ_E_SHAPE, "need rows >= 0 and columns >= 1 (got %d, %d)", rows, columns);
+    if (rows < 0 || rows > MOST_ROWS || columns < 1) return fail(MIXAQ_E_SHAPE, "need 0 <= rows <= 2^30 and columns >= 1 (got %d, %d)", rows, columns);
     if (block_rows != 1 && block_rows != SBLOCK) return fail(MIXAQ_E_SHAPE, "block_rows must be 1 or 128 (got %d)", block_rows);
     if (rows == 0) return MIXAQ_OK;
     const int32_t scale_rows = block_rows == 1 ? rows : blocks_of(rows);
@@ -163,6 +162,8 @@ extern "C" int mixaq_scaled_quantize(const mixaq_rows* x, int32_t rows, int32_t 
     if (!rc) rc = check_rows(q, "q", columns, true, scale_rows);
     if (rc) return rc;
     if (q->type != MIXAQ_E4M3) return fail(MIXAQ_E_SHAPE, "q must be codes");
-    if (rows_overlap(*x, rows, columns, *q, rows, columns)) return fail(MIXAQ_E_SHAPE, "x and q overlap");
+    const Extent from = extent_of(*x, rows, columns), codes = extent_of(*q, rows, columns), scales = scales_of(*q, scale_rows, columns);
+    if (overlap(codes, from) || overlap(scales, from)) return fail(MIXAQ_E_SHAPE, "x and q overlap");
+    if (overlap(codes, scales)) return fail(MIXAQ_E_SHAPE, "codes and scales of q overlap");
     return launch_quantize(*x, rows, columns, block_rows, *q, (hipStream_t)stream);
 }

@@ -269,6 +269,9 @@ def test_layer_refuses():
         refused(-4, "needed", x.t, y.t, workspace=ws[:-1])
         refused(-4, "aligned", x.t, y.t, workspace=torch.empty(ws.numel() + 256, dtype=torch.uint8, device="cuda")[16:])
         refused(-2, "overlap", x.t, x.t[:, :100], workspace=ws)
+        xq, yq = Room(n, 200, "e4m3"), Room(n, 100, "e4m3")
+        refused(-2, "overlap", xq.t, yq.t, x_scales=xq.scales, y_scales=xq.scales[:1])           # scales written while they are read
+        refused(-2, "workspace overlaps", x.t, yq.t, y_scales=ws.view(torch.float32)[:n].view(1, n), workspace=ws)
         large = torch.zeros(n * 512, dtype=torch.uint8, device="cuda")
         refused(-2, "workspace overlaps", large.view(torch.bfloat16)[:n * 200].view(n, 200), y.t, workspace=large)
         with pytest.raises(ValueError, match="do not fit"):

@@ -62,7 +62,7 @@ def refused(code, words, rc):
     (NULL, "x is NULL", None, 4, 200, 1, codes()),
     (NULL, "q is NULL", rows(), 4, 200, 1, codes(data=None)),
     (NULL, "scales is NULL", rows(), 4, 200, 1, codes(scales=None)),
-    (SHAPE, "rows >= 0", rows(), -1, 200, 1, codes()),
+    (SHAPE, "0 <= rows", rows(), -1, 200, 1, codes()),
     (SHAPE, "columns >= 1", rows(), 4, 0, 1, codes()),
     (SHAPE, "block_rows", rows(), 4, 200, 64, codes()),
     (SHAPE, "unknown type", rows(kind=4), 4, 200, 1, codes()),
@@ -75,7 +75,10 @@ def refused(code, words, rc):
     (SHAPE, "multiples of 16", rows(), 4, 200, 1, codes(data=FAR + 8)),
     (SHAPE, "scale_stride 63", rows(), 64, 200, 1, codes(scale_stride=63)),
     (SHAPE, "overlap", rows(), 4, 200, 1, codes(data=AT + 512)),
-    (SHAPE, "too many", rows(stride=65536), 2**31 - 1, 65536, 1, codes(data=1 << 60, stride=65536, scale_stride=2**31)),
+    (SHAPE, "overlap", rows(), 4, 200, 1, codes(scales=AT + 512)),
+    (SHAPE, "codes and scales", rows(), 4, 200, 1, codes(scales=FAR + 512)),
+    (SHAPE, "rows <= 2^30", rows(), 2**30 + 1, 200, 1, codes(scale_stride=2**31)),
+    (SHAPE, "too many", rows(stride=65536), 2**30, 65536, 1, codes(data=1 << 60, stride=65536, scales=1 << 62, scale_stride=2**31)),
 ])
 def test_quantizer_refuses(code, words, x, n, cols, block, q):
     refused(code, words, M.load().mixaq_scaled_quantize(x, n, cols, block, q, None))
@@ -112,7 +115,10 @@ def norm_call(desc=None, x=None, branch=None, y=None, out=None, n=4, gate=None, 
     (NULL, "without branch", dict(branch="none", post_norm=0, gate=AT)),
     (SHAPE, "C=0", dict(C=0)),
     (SHAPE, "C=16385", dict(C=16385)),
-    (SHAPE, "rows must not", dict(n=-1)),
+    (SHAPE, "0 <= rows", dict(n=-1)),
+    (SHAPE, "rows <= 2^30", dict(n=2**30 + 1)),
+    (SHAPE, "out and x overlap", dict(out=codes(scales=AT + 256))),
+    (SHAPE, "y and out overlap", dict(out=codes(data=FAR + (1 << 20), scales=FAR + 256))),
     (SHAPE, "post_norm: unknown", dict(post_norm=3)),
     (SHAPE, "pre_norm: unknown", dict(pre_norm=-1)),
     (SHAPE, "post_norm: eps", dict(post_eps=0.0)),
@@ -165,5 +171,7 @@ def test_binding_refuses_tensors_that_do_not_fit():
         M.mixaq_scaled_quantize(x, x, x, 2)
     with pytest.raises(ValueError, match="rows_per_gate"):
         M.make_residual_norm(200, gate=torch.zeros((3, 200)))
+    with pytest.raises(ValueError, match="pre must be one of"):
+        M.make_residual_norm(200, pre="batch")
     with pytest.raises(ValueError, match="post_gamma"):
         M.make_residual_norm(200, post="layer", post_gamma=torch.zeros(199))
