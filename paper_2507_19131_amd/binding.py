@@ -359,9 +359,9 @@ def downsample_to_device(inp, device="cuda:0"):
 
 
 # ---------------------------------------------------------------- linear layers in 8-bit float, norms between them
-def _rows(t, name, scales=None, block_rows=1):
-    """A 2-D tensor on the current device as a mixaq_rows; a float8_e4m3fn one comes with its scales, float [blocks of 128 columns, rows]
-    (with block_rows 128: [.., blocks of rows])."""
+def _rows(t, name, device, scales=None, block_rows=1):
+    """A 2-D tensor on `device` as a mixaq_rows; a float8_e4m3fn one comes with its scales, float [blocks of 128 columns, rows] (with
+    block_rows 128: [.., blocks of rows])."""
     if t is None:
         return None
     kind, shape = ROW_TYPES.get(t.dtype), t.shape
@@ -371,20 +371,22 @@ def _rows(t, name, scales=None, block_rows=1):
     row, col = t.stride()
     if col != 1 and cols > 1:
         raise ValueError("%s: the values of a row must be adjacent (strides %d, %d)" % (name, row, col))
-    _on_device(t, name)
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current device (it is on %s)" % (name, t.device))
     if rows < 2:                                          # the stride of a single row means nothing
         row = -(-cols // 16) * 16
     if kind != 3:
         if scales is not None:
             raise ValueError("%s is not float8_e4m3fn, but scales are given" % name)
-        return Rows(t.data_ptr(), row, kind, None, 0)
+        return Rows(t.data_ptr(), row, kind)
     if scales is None:
         raise ValueError("%s is float8_e4m3fn: its scales are missing" % name)
     across = (rows + block_rows - 1) // block_rows
     if scales.dtype is not torch.float32 or scales.shape != ((cols + 127) // 128, across) or (across > 1 and scales.stride(1) != 1):
         raise ValueError("%s's scales must be float32 of shape (%d, %d) with adjacent columns (got %s, %s)"
                          % (name, (cols + 127) // 128, across, scales.dtype, tuple(scales.shape)))
-    _on_device(scales, name)
+    if scales.get_device() != device:
+        raise ValueError("%s's scales must be on the current device (they are on %s)" % (name, scales.device))
     return Rows(t.data_ptr(), row, kind, scales.data_ptr(), scales.stride(0) if cols > 128 else across)
 
 
@@ -395,9 +397,15 @@ def _choice(names, value, what):
 
 
 def _on_device(t, name):
+    """The device of a tensor, which has to be the current one."""
     at = t.get_device()
     if at < 0 or at != torch._C._cuda_getDevice():
         raise ValueError("%s must be on the current device (it is on %s)" % (name, t.device))
+    return at
+
+
+def _stream_of(stream, device):
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
 
 
 def _vector(t, name, shape):
@@ -414,17 +422,18 @@ def mixaq_scaled_quantize(x, codes, scales, block_rows=1, stream=None):
     """x [rows, cols] values -> codes float8_e4m3fn [rows, cols], scales float [ceil(cols / 128), ceil(rows / block_rows)]."""
     if block_rows not in (1, 128):
         raise ValueError("block_rows must be 1 or 128 (got %r)" % (block_rows,))
-    if tuple(codes.shape) != tuple(x.shape):
+    if codes.shape != x.shape:
         raise ValueError("codes have the shape %s, x %s" % (tuple(codes.shape), tuple(x.shape)))
-    a, q = _rows(x, "x"), _rows(codes, "codes", scales, block_rows)
-    _check(load().mixaq_scaled_quantize(a, x.shape[0], x.shape[1], block_rows, q, _stream(stream)))
+    at = _on_device(x, "x")
+    a, q = _rows(x, "x", at), _rows(codes, "codes", at, scales, block_rows)
+    _check(load().mixaq_scaled_quantize(a, x.shape[0], x.shape[1], block_rows, q, _stream_of(stream, at)))
     return codes, scales
 
 
 def mixaq_scaled_linear_create(w, s_w, bias=None, activation="none", stream=None):
     """w: float8_e4m3fn [N, K], s_w: float [ceil(K / 128), ceil(N / 128)] as of mixaq_scaled_quantize with block_rows 128; bias: float [N]
     or None; activation: "none" or "gelu".  Returns an opaque handle; w, s_w and bias may be released."""
-    p = ScaledLinearParams(_rows(w, "w", s_w, 128), _ptr(_vector(bias, "bias", (w.shape[0],))))
+    p = ScaledLinearParams(_rows(w, "w", _on_device(w, "w"), s_w, 128), _ptr(_vector(bias, "bias", (w.shape[0],))))
     d = ScaledLinearDesc(w.shape[1], w.shape[0], _choice(ACTIVATIONS, activation, "activation"))
     out = C.c_void_p()
     _check(load().mixaq_scaled_linear_create(C.byref(d), C.byref(p), _stream(stream), C.byref(out)))
@@ -447,12 +456,14 @@ def mixaq_scaled_linear_forward(h, x, y, x_scales=None, y_scales=None, workspace
     rows = x.shape[0]
     if x.shape[1:] != (h.K,) or y.shape != (rows, h.N):
         raise ValueError("x %s, y %s do not fit a layer of %d inputs and %d outputs" % (tuple(x.shape), tuple(y.shape), h.K, h.N))
-    a, b = _rows(x, "x", x_scales), _rows(y, "y", y_scales)
+    at = _on_device(x, "x")
+    a, b = _rows(x, "x", at, x_scales), _rows(y, "y", at, y_scales)
     ws, n = None, 0
     if workspace is not None:
-        _on_device(workspace, "workspace")
+        if workspace.get_device() != at:
+            raise ValueError("workspace must be on the current device (it is on %s)" % workspace.device)
         ws, n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(load().mixaq_scaled_linear_forward(h, a, rows, b, ws, n, _stream(stream)))
+    _check(load().mixaq_scaled_linear_forward(h, a, rows, b, ws, n, _stream_of(stream, at)))
     return y
 
 
@@ -488,9 +499,9 @@ def mixaq_residual_norm(norm, x, branch=None, y=None, out=None, out_scales=None,
         raise ValueError("x, branch, y and out must be of shape %s (got %s)" % (shape, [None if t is None else tuple(t.shape) for t in (x, branch, y, out)]))
     if rows > norm.most_rows:
         raise ValueError("%d rows, but the gate has vectors for %d" % (rows, norm.most_rows))
-    desc, params = norm.args
-    _check(load().mixaq_residual_norm(desc, params, _rows(x, "x"), _rows(branch, "branch"), _rows(y, "y"), _rows(out, "out", out_scales), rows,
-                                      _stream(stream)))
+    (desc, params), at = norm.args, _on_device(x, "x")
+    _check(load().mixaq_residual_norm(desc, params, _rows(x, "x", at), _rows(branch, "branch", at), _rows(y, "y", at),
+                                      _rows(out, "out", at, out_scales), rows, _stream_of(stream, at)))
     return y, out
 
 

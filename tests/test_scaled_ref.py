@@ -162,11 +162,11 @@ def test_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(ValueError, match="current device|CUDA|device"):
         M.mixaq_scaled_quantize(x, torch.zeros((4, 208), dtype=torch.uint8).view(torch.float8_e4m3fn)[:, :200], torch.zeros((2, 4)))
     with pytest.raises(ValueError, match="2-D"):
-        M._rows(x.double(), "x")
+        M._rows(x.double(), "x", 0)
     with pytest.raises(ValueError, match="2-D"):
-        M._rows(x[0], "x")
+        M._rows(x[0], "x", 0)
     with pytest.raises(ValueError, match="adjacent"):
-        M._rows(x.t(), "x")
+        M._rows(x.t(), "x", 0)
     with pytest.raises(ValueError, match="block_rows"):
         M.mixaq_scaled_quantize(x, x, x, 2)
     with pytest.raises(ValueError, match="rows_per_gate"):
