@@ -706,7 +706,7 @@ int launch_split(const LinearArgs& A, hipStream_t st)
     return MIXAQ_OK;
 }
 
-// Which kernel takes a product: by rows, K, N and how sums are taken, never by x's type or by whether exact sums become codes, so that values
+// Which kernel takes a product: by rows, the layer and how sums are taken, never by x's type or by whether exact sums become codes, so that values
 // in and codes out are the same results.  us (graph replays; few / split / tile / large):
 //   FEW while its workgroups - 16 rows and 16 outputs each - times their blocks of K stay few, and for up to 16 rows:
 //     64 x 1024 x 1024 3.2 / 7.1    128 x 4096 x 1024 7.3 / 16.8    256 x 1024 x 1024 4.9 / 7.2    1001 x 1000 x 333 5.8 / 7.2    64 x 4096 x 4096
@@ -714,7 +714,9 @@ int launch_split(const LinearArgs& A, hipStream_t st)
 //   SPLIT below 96 tiles of 128 x 128, codes out: 1024 x 1024 x 1024 8.9 / 10.9 (tile)    1024 x 4096 x 1024 21.4 / 39.3 |  4704 x 1536 x 384 (111 tiles)
 //     21.8 / 17.6    8192 x 256 x 256 (128) 10.6 / 5.7; bf16 out the same or 5 % to either side at 64
 //   LARGE, 16-bit sums, from 192 tiles of 256 x 256 and two blocks of K: 16384 x 512 x 512 (128) 11.3 (tile) / 13.9    2048 x 1024 x 4096 (128)
-//     15.4 / 19.0 |  16384 x 768 x 768 (192) 18.7 / 17.4    8192 x 256 x 2048 (256) 14.2 / 12.8    4096 x 2048 x 4096 (256) 43.9 / 34.9
+//     15.4 / 19.0 |  16384 x 768 x 768 (192) 18.7 / 17.4    8192 x 256 x 2048 (256) 14.2 / 12.8    4096 x 2048 x 4096 (256) 43.9 / 34.9; with a
+//     GELU, which a second workgroup on the CU hides, from six blocks: 16384 x 384 x 1536 28.4 (tile) / 33.8    100000 x 256 x 1024 108 / 115 |
+//     16384 x 1024 x 2048 57.7 / 52.2
 //   LARGE, exact sums, from 224 tiles of 256 x 128 and three blocks: 4096 x 4096 x 1024 (128) 42.6 (tile) / 50.9    65536 x 256 x 1024 (two blocks)
 //     56.1 / 60.8 |  4704 x 384 x 1536 (228) 10.8 / 10.4    8192 x 1024 x 1024 (256) 22.4 / 19.7    16384 x 1024 x 2048 75.3 / 70.2
 enum Form { FORM_FEW, FORM_SPLIT, FORM_TILE, FORM_LARGE };
@@ -724,7 +726,7 @@ Form form_of(int M, const mixaq_scaled_linear* h, bool exact, long long ldx)
     const long long large = (M + 255LL) / 256 * (exact ? h->NB : (h->NB + 1) / 2);
     if (M <= 16 || tiles16 * h->KB <= 5000 + 1400LL * h->KB) return FORM_FEW;
     if (tiles128 < 96 || ldx >= (1 << 22)) return FORM_SPLIT;                 // (rows 4 MB apart: the tiles count in 32 bits)
-    return large >= (exact ? 224 : 192) && h->KB >= (exact ? 3 : 2) ? FORM_LARGE : FORM_TILE;
+    return large >= (exact ? 224 : 192) && h->KB >= (exact ? 3 : h->d.activation ? 6 : 2) ? FORM_LARGE : FORM_TILE;
 }
 
 template <int XT, int YT>

@@ -121,6 +121,44 @@ def test_a_single_value_per_row_far_apart():
     assert np.all(np.abs(as64(y) - want) <= R.allowed(want, bound, "f16"))
 
 
+def far_rows(rows, cols, kind, stride):
+    """Rows whose offsets pass 2^31 bytes and values, in memory that is not filled."""
+    es = {"f32": 4, "f16": 2, "bf16": 2, "e4m3": 1}[kind]
+    return torch.empty(rows * stride * es, dtype=torch.uint8, device="cuda").view(TYPES[kind]).as_strided((rows, cols), (stride, 1))
+
+
+@pytest.mark.parametrize("K", [128, 257])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_many_rows_beyond_32_bit_offsets(K, kind):
+    """Both tiled kernels, of either kind of sums; compared on rows from everywhere."""
+    rows, N = 40000, 512
+    with Layer(90, N, K) as layer:
+        v = values(91, 2000, K).repeat(20, 1)
+        x, scales = far_rows(rows, K, "e4m3", 65552), torch.empty((R.blocks(K), rows), device="cuda")
+        M.mixaq_scaled_quantize(v.cuda(), x, scales)
+        y = far_rows(rows, N, kind, 65536)
+        ys = torch.empty((4, rows), device="cuda") if kind == "e4m3" else None
+        M.mixaq_scaled_linear_forward(layer.h, x, y, x_scales=scales, y_scales=ys)
+        at = torch.tensor([0, 1, 255, 256, 20000, 32767, 32768, 32769, 36000, 39998, 39999])
+        codes, s64 = R.quantize(v[at].numpy())
+        assert np.array_equal(as64(scales[:, at.cuda()]), s64)
+        room = Room(len(at), N, kind)
+        room.t.copy_(torch.stack([y[int(i)] for i in at]) if kind != "e4m3" else torch.stack([y[int(i)].view(torch.uint8) for i in at]).view(torch.float8_e4m3fn))
+        if kind == "e4m3":
+            room.scales.copy_(ys[:, at.cuda()])
+        check_result(room, *layer.reference(R.dequantize(codes, s64), kind), kind)
+
+
+def test_norms_of_many_rows_beyond_32_bit_offsets():
+    rows, C = 40000, 96
+    x, out = far_rows(rows, C, "bf16", 65536), far_rows(rows, C, "bf16", 65536)
+    v = values(92, rows, C).bfloat16()
+    x.copy_(v.cuda())
+    M.mixaq_residual_norm(M.make_residual_norm(C), x, None, None, out)
+    want, bound = R.norm(as64(v), "layer", float(np.float32(1e-5)), None, None, np.zeros((rows, C)))
+    assert np.all(np.abs(as64(out) - want) <= R.allowed(want, bound, "bf16"))
+
+
 # ---------------------------------------------------------------- linear layer
 class Layer:
     def __init__(self, seed, N, K, bias=True, activation="none", w=None):
