@@ -729,6 +729,15 @@ Form form_of(int M, const mixaq_scaled_linear* h, bool exact, long long ldx)
     return large >= (exact ? 224 : 192) && h->KB >= (exact ? 3 : h->d.activation ? 6 : 2) ? FORM_LARGE : FORM_TILE;
 }
 
+// Whether values are quantized on their way into FEW's product: every workgroup does it for its 16 rows, so with many workgroups or blocks a launch of
+// its own is shorter.  us of the GPU, f32 / bf16 values, in one launch and in two (the second takes the host another 3.5):
+//     1 x 1024 x 4096 3.3 / 3.5, 4.8    64 x 1024 x 1024 4.7 / 4.1, 6.0    1 x 4096 x 4096 6.1 / 6.8, 6.1    256 x 1024 x 1024 10.5 / 7.8, 7.9 |
+//     16 x 8192 x 1024 17 / 11, 10    1001 x 1000 x 333 21 / 13, 11    64 x 4096 x 4096 33 / 21, 15
+bool quantized_inside(int M, const mixaq_scaled_linear* h)
+{
+    return form_of(M, h, true, 0) == FORM_FEW && h->KB <= 32 && (M + 15LL) / 16 * h->NB * 8 * h->KB <= 8192;       // (FEW whatever the sums)
+}
+
 template <int XT, int YT>
 int launch_few(const LinearArgs& A, hipStream_t st)
 {
@@ -760,7 +769,7 @@ size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 // the workspace: codes and scales of x, where it is given as values and not quantized on its way into the product
 size_t workspace_of(const mixaq_scaled_linear* h, int32_t rows, int32_t x_type)
 {
-    if (x_type == MIXAQ_E4M3 || rows == 0 || form_of(rows, h, true, 0) == FORM_FEW) return 0;      // (FEW whatever the sums)
+    if (x_type == MIXAQ_E4M3 || rows == 0 || quantized_inside(rows, h)) return 0;
     return align256((size_t)rows * round_up16(h->d.K)) + align256((size_t)rows * h->KB * 4);
 }
 

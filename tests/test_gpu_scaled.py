@@ -219,7 +219,7 @@ def test_layer(rows, K, N, x_kind, y_kind):
         assert y.untouched()
 
 
-@pytest.mark.parametrize("rows,K,N", [(1, 1024, 512), (40, 384, 200), (70, 200, 384), (300, 512, 300), (2000, 256, 640), (3001, 200, 600), (6200, 300, 2000)])
+@pytest.mark.parametrize("rows,K,N", [(1, 1024, 512), (40, 384, 200), (70, 200, 384), (300, 512, 300), (1, 4200, 64), (900, 300, 500), (2000, 256, 640), (3001, 200, 600), (6200, 300, 2000)])
 @pytest.mark.parametrize("activation", ["none", "gelu"])
 def test_values_and_codes_are_two_forms_of_one_call(rows, K, N, activation):
     """Values in: the result of quantizing them first.  Codes out: the 32-bit result quantized."""
