@@ -7,8 +7,6 @@
 #include <new>
 #include <type_traits>
 
-#include "arena.h"
-
 using namespace mixaq;
 
 struct mixaq_scaled_linear {
@@ -72,9 +70,8 @@ __global__ __launch_bounds__(256) void pack_vectors_kernel(const float* s, long 
 
 // ---- the end of a tile ------------------------------------------------------------------------------------------------
 // GELU(v) = v Phi(v), Phi(v) = 1 / (1 + 2^-t), t = v P(v^2): the logarithm of Phi's odds is odd and smooth, P its fit by weighted least
-// squares on 0 < v < 7 (at most 9.4e-8 |v| off; beyond, t only grows).  19 issue slots with the two quarter-rate instructions at four each;
-// by Abramowitz and Stegun's erfc, which is as exact, 25.  The median keeps the last product at -infinity from being 0 times infinity; a NaN
-// comes through the other factor.
+// squares on 0 < v < 7 (at most 9.4e-8 |v| off; beyond, t only grows).  13 instructions, by Abramowitz and Stegun's erfc, which is as exact,
+// 18.  The median keeps the last product at -infinity from being 0 times infinity; a NaN comes through the other factor.
 __device__ __forceinline__ float gelu(float v)
 {
     const float u = v * v;
@@ -91,9 +88,9 @@ __device__ __forceinline__ float gelu(float v)
 
 // The end of a wave's ROWS rows and 128 outputs: a lane holds those of one row, the bias in them, in RUNS runs of 16 neighbouring ones, run i from
 // column offset(i) of block nb on; the lanes l, l + ROWS, .. hold the whole row.  Through LDS (`turn`: 16 or 32 rows x 256 bytes of the
-// wave's own), so that a store covers whole lines: from the lanes themselves it would touch 32 rows with 32 bytes each (268324 x 128 x 512 of bf16 115
-// instead of 90 us, 100000 x 96 x 384 of f32 66 instead of 35).  Its 16-byte pieces are turned by the row, so that neither side meets a bank twice.  The last block of a row that ends
-// inside it is stored value by value.
+// wave's own), so that a store covers whole lines: from the lanes themselves it would touch 32 rows with 32 bytes each (268324 x 128 x 512 of bf16
+// 115 us instead of 90, 100000 x 96 x 384 of f32 66 instead of 35).  Its 16-byte pieces are turned by the row, so that neither side meets a
+// bank twice.  A block that ends beyond N is stored value by value.
 template <int YT, int RUNS, int ROWS, typename Offset>
 __device__ __forceinline__ void finish(const LinearArgs& A, float (&v)[16 * RUNS], int nb, long long row0, v4i* turn, Offset offset)
 {
@@ -216,7 +213,9 @@ __device__ __forceinline__ v4f product(v4i w0, v4i w1, v4i x0, v4i x1)
 // A workgroup of NW waves computes 16 MR rows times NR tiles of 16 outputs, wave w the blocks w, w + NW, .. of K; the waves' sums meet in LDS,
 // in the order of the waves.  For products of few tiles: a lone row at K = 1024 is one round trip to memory.  A block's scale meets
 // its product where both are of one row, so x may be given as values: a lane holds 32 of the 128 values of its row, the other three
-// lanes of the row the rest, and what it needs as operand is the codes of its own.
+// lanes of the row the rest, and what it needs as operand is the codes of its own.  What bounds it: a launch and two round trips (1 x 1024 x 4096
+// 2.7 us from codes, 3.4 from values; 4.2 MB of weights would take 0.8), with more rows the operands' way through the caches, each workgroup for
+// itself (64 x 4096 x 4096 11.4 us: 67 MB of weights and as much of x, 12 TB/s).
 template <int XT>
 __device__ __forceinline__ void operand_of(const LinearArgs& A, int row, int kb, int g, v4i (&x)[2], float& scale)
 {
@@ -374,12 +373,14 @@ __global__ __launch_bounds__(NW * 64) void split_kernel(LinearArgs A, int row_ti
 
 // ---- both operands through LDS ------------------------------------------------------------------------------------------
 // A workgroup of WM x WN waves computes 32 MT WM rows times 128 WN outputs, a wave 32 MT rows times one block of 128 outputs: the product of a
-// block's two scales is then a value per lane, and a row's codes need no exchange but between the two halves of a wave.  K goes in stages
+// block's two scales is then a value per lane, and a row's codes need no exchange beyond the wave.  K goes in stages
 // of one block of 128 through two LDS buffers filled by direct loads; a stage travels under the products of the one before it.
 // Rows of x lie in LDS as 8 chunks of 16 bytes whose places are turned by half the row's number, so that the 16 lanes that are served
 // together (16 rows, one chunk) meet all 64 banks.
-// The direct loads are asm: as a builtin every LDS read behind them waits for all of them.
-// Nothing for stages from `end` on, which the asm finds out: a branch around it would be one in the middle of a stage.
+// What bounds it: of 16384 x 4096 x 3840 to bf16 (240 to 280 us by card, 2.1 PFLOP/s; a library product without scales 2.4) the matrix instructions are
+// busy in 52 % of the clocks and vector instructions in 41 %, and beside operands of 16 x 16 x 128 they hardly overlap; of codes out the vector
+// instructions (61 %, with a GELU at K = 128 82 %).
+// The direct loads are asm: as a builtin every LDS read behind them waits for all of them.  They do nothing for stages from `end` on, which the asm finds out: a branch around it would be one in the middle of a stage.
 #define MIXAQ_REQUEST(SIZE_)                                                                                                              \
     int m0; /* given back: the compiler does not let an asm statement change it */                                                       \
     asm volatile("s_cmp_ge_i32 %4, %5\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_" SIZE_ \
@@ -391,22 +392,16 @@ __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigne
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-// one half of a product of a block: the chunks 2 HALF and 2 HALF + 1 of a lane
-template <bool EXACT, int HALF>
+// one half of an exact product of a block: the chunks 2 HALF and 2 HALF + 1 of a lane
+template <int HALF>
 __device__ __forceinline__ v16f half_product(const v4i (&w)[4], const v4i (&x)[4], v16f d)
 {
-    if constexpr (EXACT) {
 #pragma unroll
-        for (int j = 2 * HALF; j < 2 * HALF + 2; ++j) {
-            d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][0], w[j][1]), widen(x[j][0], x[j][1]), d, 0, 0, 0);
-            d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][2], w[j][3]), widen(x[j][2], x[j][3]), d, 0, 0, 0);
-        }
-        return d;
-    } else {
-        const v8i a = __builtin_shufflevector(w[2 * HALF], w[2 * HALF + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-        const v8i b = __builtin_shufflevector(x[2 * HALF], x[2 * HALF + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, 0, 0, 0, 0, 0, 0);
+    for (int j = 2 * HALF; j < 2 * HALF + 2; ++j) {
+        d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][0], w[j][1]), widen(x[j][0], x[j][1]), d, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen(w[j][2], w[j][3]), widen(x[j][2], x[j][3]), d, 0, 0, 0);
     }
+    return d;
 }
 
 // Of instructions of 32 x 32 the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, and lane half h takes the 16-byte chunks h, 2 + h, 4 + h
@@ -643,10 +638,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void tile_kernel(LinearArgs A, int
                     read_w(kb + 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                d[p & 1] = half_product<EXACT, 0>(w[T & 1], x[m], (v16f){});
+                d[p & 1] = half_product<0>(w[T & 1], x[m], (v16f){});
                 add(last, d[(p & 1) ^ 1], scale, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                d[p & 1] = half_product<EXACT, 1>(w[T & 1], x[m], d[p & 1]);
+                d[p & 1] = half_product<1>(w[T & 1], x[m], d[p & 1]);
                 add(last, d[(p & 1) ^ 1], scale, 1);
                 __builtin_amdgcn_sched_barrier(0);
                 if (T == 3 && m == MT - 1) s_last = s[m];

@@ -60,7 +60,7 @@ struct QuantArgs {
 };
 
 // One block of a row is 16 lanes with eight values each; a wave takes 16 rows of one block of columns, four at a time, and the waves
-// beside it the next blocks of the same rows.
+// beside it the next blocks of the same rows.  What bounds it is memory: 68208 x 384 of bf16 14.7 us, 5.4 TB/s.
 template <typename T, bool TINY>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs A)
 {
@@ -83,7 +83,8 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs A)
     }
 }
 
-// A workgroup per 128 x 128 tile, held in registers between its maximum and its codes.
+// A workgroup per 128 x 128 tile, held in registers between its maximum and its codes: one read of the values.  4000 x 1000 of f32 6.6 us, a tile
+// a CU: the launch, a round trip of 64 KB, the maximum's and the stores; more tiles overlap.
 template <typename T, bool TINY>
 __global__ __launch_bounds__(256) void quantize_tiles_kernel(QuantArgs A)
 {
