@@ -195,10 +195,11 @@ template <int TX, int TB, int G, int V, bool TINY = false>
 void launch(const NormArgs& A, hipStream_t st)
 {
     // Three workgroups a CU, each on every 768th group of rows: neighbouring rows are on their way at one time.  8190 x 4096 values of bf16 with
-    // gates, us: 512 workgroups 68, 768 61, 1024 73, 2048 67, 4096 71; a run of neighbouring rows for each of 1024 73.
+    // gates, us: 512 workgroups 68, 768 61, 1024 73, 2048 67, 4096 71; a run of neighbouring rows for each of 1024 73.  Up to 64 values, which are few
+    // bytes a turn, 2048: 200000 x 64 38 instead of 43, 260000 x 128 68 instead of 60.
     constexpr int ROWS = G < 256 ? 256 / G : 1;
     const long long groups = ((long long)A.rows + ROWS - 1) / ROWS;
-    hipLaunchKernelGGL((residual_norm_kernel<TX, TB, G, V, TINY>), dim3((unsigned)std::min(groups, 768LL)), dim3(G < 256 ? 256 : G), 0, st, A);
+    hipLaunchKernelGGL((residual_norm_kernel<TX, TB, G, V, TINY>), dim3((unsigned)std::min(groups, A.C <= 64 ? 2048LL : 768LL)), dim3(G < 256 ? 256 : G), 0, st, A);
 }
 // The lanes of a row: 16, a wave, then a workgroup of four or sixteen, with one or two times eight values each.  (us, bf16, with gates:  C = 256
 // in 16 lanes of two 60, in 64 of one 88;  1024 in 64 of two 61, in 256 of one 105;  4096 in 256 of two 60, in 512 of one 71;  8192 in 512 of
