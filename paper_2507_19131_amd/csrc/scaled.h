@@ -143,7 +143,7 @@ __device__ __forceinline__ unsigned max16(unsigned m) { return over16(m, MaxOf()
 constexpr long long MOST_THREADS = 1LL << 32;      // of one launch
 
 inline int size_of(int type) { return type == MIXAQ_F32 ? 4 : type == MIXAQ_E4M3 ? 1 : 2; }
-inline int blocks_of(int columns) { return (columns + SBLOCK - 1) / SBLOCK; }
+inline int blocks_of(int columns) { return (columns - 1) / SBLOCK + 1; }       // of at least one; up to the largest int
 
 // The matrix `m` as an argument called `name`: `columns` values or codes a row, scales for `scale_rows` rows.
 int check_rows(const mixaq_rows* m, const char* name, int32_t columns, bool codes_allowed, int32_t scale_rows);
