@@ -84,6 +84,7 @@ class ResidualNormParams(C.Structure):
 ROW_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
 ACTIVATIONS = {"none": 0, "gelu": 1}
 NORMS = {"none": 0, "layer": 1, "rms": 2}
+MOST_INT = 2**31 - 1
 
 
 def lib_path():
@@ -368,6 +369,8 @@ def _rows(t, name, device, scales=None, block_rows=1):
     if kind is None or len(shape) != 2:
         raise ValueError("%s must be a 2-D tensor of float32, float16, bfloat16 or float8_e4m3fn" % name)
     rows, cols = shape
+    if rows > MOST_INT or cols > MOST_INT:                # (ctypes would cut them to 32 bits)
+        raise ValueError("%s is %d x %d: calls take up to 2^30 rows of less than 2^31 columns" % (name, rows, cols))
     row, col = t.stride()
     if col != 1 and cols > 1:
         raise ValueError("%s: the values of a row must be adjacent (strides %d, %d)" % (name, row, col))
@@ -446,6 +449,8 @@ def mixaq_scaled_linear_destroy(h):
 
 
 def mixaq_scaled_linear_workspace_bytes(h, rows, x_dtype, y_dtype):
+    if rows > MOST_INT:
+        raise ValueError("calls take up to 2^30 rows (got %d)" % rows)
     n = C.c_size_t()
     _check(load().mixaq_scaled_linear_workspace_bytes(h, rows, ROW_TYPES[x_dtype], ROW_TYPES[y_dtype], C.byref(n)))
     return n.value
@@ -472,7 +477,7 @@ class ResidualNorm:
 
     def __init__(self, desc, params, vectors, most_rows):
         self.desc, self.params, self.vectors = desc, params, vectors
-        self.channels, self.most_rows = desc.C, most_rows             # most_rows: that the gate's vectors are enough for
+        self.channels, self.most_rows = desc.C, most_rows             # most_rows: that the gate's vectors are enough for, or None
         self.args = C.byref(desc), C.byref(params)
 
 
@@ -480,16 +485,20 @@ def make_residual_norm(channels, post="none", pre="layer", eps=1e-5, residual_sc
                        pre_beta=None, gate=None, rows_per_gate=None):
     """post, pre: "none", "layer" or "rms"; gammas and betas: float [C] or None; gate: float [C] for all rows, or [G, C] with a vector for
     every rows_per_gate rows."""
+    if not 1 <= channels <= MOST_INT:
+        raise ValueError("channels must be positive and below 2^31 (got %d)" % channels)
     if gate is not None:
         gate = gate.unsqueeze(0) if gate.dim() == 1 else gate
         if rows_per_gate is None and gate.shape[0] != 1:
             raise ValueError("gate has %d rows: rows_per_gate is missing" % gate.shape[0])
+        if rows_per_gate is not None and rows_per_gate < 1:
+            raise ValueError("rows_per_gate must be positive (got %s)" % rows_per_gate)
         _vector(gate, "gate", (gate.shape[0], channels))
     vectors = [_vector(v, n, (channels,)) for v, n in ((post_gamma, "post_gamma"), (post_beta, "post_beta"), (pre_gamma, "pre_gamma"),
                                                        (pre_beta, "pre_beta"))] + [gate]
-    span = 2**31 - 1 if rows_per_gate is None else int(rows_per_gate)
-    desc = ResidualNormDesc(channels, _choice(NORMS, post, "post"), _choice(NORMS, pre, "pre"), span, eps, eps, residual_scale)
-    return ResidualNorm(desc, ResidualNormParams(*[_ptr(v) for v in vectors]), vectors, 2**31 - 1 if gate is None else gate.shape[0] * span)
+    span = MOST_INT if rows_per_gate is None else int(rows_per_gate)
+    desc = ResidualNormDesc(channels, _choice(NORMS, post, "post"), _choice(NORMS, pre, "pre"), min(span, MOST_INT), eps, eps, residual_scale)
+    return ResidualNorm(desc, ResidualNormParams(*[_ptr(v) for v in vectors]), vectors, None if gate is None else gate.shape[0] * span)
 
 
 def mixaq_residual_norm(norm, x, branch=None, y=None, out=None, out_scales=None, stream=None):
@@ -497,7 +506,7 @@ def mixaq_residual_norm(norm, x, branch=None, y=None, out=None, out_scales=None,
     shape = rows, _ = x.shape[0], norm.channels
     if x.shape != shape or (branch is not None and branch.shape != shape) or (y is not None and y.shape != shape) or (out is not None and out.shape != shape):
         raise ValueError("x, branch, y and out must be of shape %s (got %s)" % (shape, [None if t is None else tuple(t.shape) for t in (x, branch, y, out)]))
-    if rows > norm.most_rows:
+    if norm.most_rows is not None and rows > norm.most_rows:
         raise ValueError("%d rows, but the gate has vectors for %d" % (rows, norm.most_rows))
     (desc, params), at = norm.args, _on_device(x, "x")
     _check(load().mixaq_residual_norm(desc, params, _rows(x, "x", at), _rows(branch, "branch", at), _rows(y, "y", at),

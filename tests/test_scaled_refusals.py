@@ -30,3 +30,62 @@ rc = M.load().mixaq_scaled_quantize(x, n, %d, 1, q, None)
 assert rc == -2 and b"too many" in M.load().mixaq_last_error(), (rc, M.load().mixaq_last_error())
 """ % (ROOT, AT, FAR, FAR << 1, columns)
     subprocess.run([sys.executable, "-c", code], check=True, timeout=120)
+
+
+# ---------------------------------------------------------------- the binding, on CPU tensors, with nothing called behind it
+@pytest.fixture
+def calls(monkeypatch):
+    """What the binding passes on to the library, by name; the tensors' device is taken for the current one."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: made.append((name, a)) or 0
+
+    monkeypatch.setattr(M, "load", Library)
+    monkeypatch.setattr(M, "_on_device", lambda t, name: t.get_device())
+    monkeypatch.setattr(M, "_stream_of", lambda stream, device: None)
+    monkeypatch.setattr(M, "_stream", lambda stream: None)
+    return made
+
+
+def e4m3(rows, cols):
+    return torch.zeros((1, 1), dtype=torch.uint8).view(torch.float8_e4m3fn).expand(rows, cols) if rows > 1000 or cols > 1000 else M.alloc_codes(rows, cols, device="cpu")[0]
+
+
+def layer(K, N):
+    h = C.c_void_p(0)
+    h.K, h.N = K, N
+    return h
+
+
+@pytest.mark.parametrize("rows", [2**31, 2**32 + 3, 2**33])
+def test_more_rows_than_the_library_counts_are_refused(calls, rows):
+    """What passes 32 bits would arrive as another number of rows."""
+    x, scales = torch.zeros((1, 8)).expand(rows, 8), torch.zeros((1, 1)).expand(1, rows)
+    norm = M.make_residual_norm(8)
+    for call in (lambda: M.mixaq_scaled_quantize(x, e4m3(rows, 8), scales), lambda: M.mixaq_scaled_linear_forward(layer(8, 8), x, x),
+                 lambda: M.mixaq_residual_norm(norm, x, out=x), lambda: M.mixaq_scaled_linear_workspace_bytes(layer(8, 8), rows, torch.float32, torch.float32)):
+        with pytest.raises(ValueError, match="2\\^30 rows"):
+            call()
+    assert not calls
+
+
+def test_wider_matrices_than_the_library_counts_are_refused(calls):
+    cols = 2**32 + 8                                      # (no such matrix is allocated: its values would be one, 0 apart)
+    wide = torch.zeros((1, 1)).expand(1, cols)
+    with pytest.raises(ValueError):
+        M.mixaq_scaled_quantize(wide, e4m3(1, cols), torch.zeros((1, 1)).expand(cols // 128 + 1, 1))
+    with pytest.raises(ValueError, match="channels"):
+        M.make_residual_norm(cols)
+    assert not calls
+
+
+def test_a_gate_for_more_rows_than_there_can_be_is_a_gate_for_all(calls):
+    x = torch.zeros((5, 8))
+    for span in (2**31 - 1, 2**31, 2**32, 2**32 + 3, 2**63):
+        norm = M.make_residual_norm(8, gate=torch.ones(1, 8), rows_per_gate=span)
+        assert norm.desc.rows_per_gate == 2**31 - 1
+        M.mixaq_residual_norm(norm, x, x, out=x)
+    with pytest.raises(ValueError, match="rows_per_gate"):
+        M.make_residual_norm(8, gate=torch.ones(1, 8), rows_per_gate=-1)
