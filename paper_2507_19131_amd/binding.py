@@ -479,6 +479,7 @@ class ResidualNorm:
         self.desc, self.params, self.vectors = desc, params, vectors
         self.channels, self.most_rows = desc.C, most_rows             # most_rows: that the gate's vectors are enough for, or None
         self.args = C.byref(desc), C.byref(params)
+        self.device = next((v.get_device() for v in vectors if v is not None), None)      # None: no vectors
 
 
 def make_residual_norm(channels, post="none", pre="layer", eps=1e-5, residual_scale=1.0, post_gamma=None, post_beta=None, pre_gamma=None,
@@ -509,6 +510,8 @@ def mixaq_residual_norm(norm, x, branch=None, y=None, out=None, out_scales=None,
     if norm.most_rows is not None and rows > norm.most_rows:
         raise ValueError("%d rows, but the gate has vectors for %d" % (rows, norm.most_rows))
     (desc, params), at = norm.args, _on_device(x, "x")
+    if norm.device is not None and norm.device != at:
+        raise ValueError("x is on %s, but the norm's vectors are on device %d" % (x.device, norm.device))
     _check(load().mixaq_residual_norm(desc, params, _rows(x, "x", at), _rows(branch, "branch", at), _rows(y, "y", at),
                                       _rows(out, "out", at, out_scales), rows, _stream_of(stream, at)))
     return y, out

@@ -89,3 +89,19 @@ def test_a_gate_for_more_rows_than_there_can_be_is_a_gate_for_all(calls):
         M.mixaq_residual_norm(norm, x, x, out=x)
     with pytest.raises(ValueError, match="rows_per_gate"):
         M.make_residual_norm(8, gate=torch.ones(1, 8), rows_per_gate=-1)
+
+
+def test_a_norm_takes_rows_on_the_device_of_its_vectors(calls, monkeypatch):
+    """Its vectors were on the current device when it was made; another one may be current when it is called."""
+    with_gate, bare = M.make_residual_norm(8, gate=torch.ones(8)), M.make_residual_norm(8)
+    gamma = M.make_residual_norm(8, pre_gamma=torch.ones(8))
+    beta = M.make_residual_norm(8, post="layer", post_beta=torch.ones(8))
+    monkeypatch.setattr(M, "_on_device", lambda t, name: 1)
+    monkeypatch.setattr(M, "_rows", lambda *a: None)      # (x, y on device 1)
+    x = torch.zeros((5, 8))
+    for norm in (with_gate, gamma, beta):
+        with pytest.raises(ValueError, match="vectors"):
+            M.mixaq_residual_norm(norm, x, x, out=x)
+    assert not calls
+    M.mixaq_residual_norm(bare, x, x, out=x)              # without vectors it belongs to no device
+    assert len(calls) == 1
