@@ -408,7 +408,11 @@ def _on_device(t, name):
 
 
 def _stream_of(stream, device):
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+    if stream is None:
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(device))
+    if stream.device_index != device:
+        raise ValueError("the stream must be one of the current device (it is one of device %d)" % stream.device_index)
+    return C.c_void_p(stream.cuda_stream)
 
 
 def _vector(t, name, shape):
@@ -436,10 +440,11 @@ def mixaq_scaled_quantize(x, codes, scales, block_rows=1, stream=None):
 def mixaq_scaled_linear_create(w, s_w, bias=None, activation="none", stream=None):
     """w: float8_e4m3fn [N, K], s_w: float [ceil(K / 128), ceil(N / 128)] as of mixaq_scaled_quantize with block_rows 128; bias: float [N]
     or None; activation: "none" or "gelu".  Returns an opaque handle; w, s_w and bias may be released."""
-    p = ScaledLinearParams(_rows(w, "w", _on_device(w, "w"), s_w, 128), _ptr(_vector(bias, "bias", (w.shape[0],))))
+    at = _on_device(w, "w")
+    p = ScaledLinearParams(_rows(w, "w", at, s_w, 128), _ptr(_vector(bias, "bias", (w.shape[0],))))
     d = ScaledLinearDesc(w.shape[1], w.shape[0], _choice(ACTIVATIONS, activation, "activation"))
     out = C.c_void_p()
-    _check(load().mixaq_scaled_linear_create(C.byref(d), C.byref(p), _stream(stream), C.byref(out)))
+    _check(load().mixaq_scaled_linear_create(C.byref(d), C.byref(p), _stream_of(stream, at), C.byref(out)))
     out.K, out.N = w.shape[1], w.shape[0]
     return out
 

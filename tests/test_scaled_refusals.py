@@ -105,3 +105,12 @@ def test_a_norm_takes_rows_on_the_device_of_its_vectors(calls, monkeypatch):
     assert not calls
     M.mixaq_residual_norm(bare, x, x, out=x)              # without vectors it belongs to no device
     assert len(calls) == 1
+
+
+def test_a_stream_of_another_device_is_refused(monkeypatch):
+    class Stream:
+        device_index, cuda_stream = 1, 0x1234
+
+    assert M._stream_of(Stream, 1).value == 0x1234
+    with pytest.raises(ValueError, match="stream"):
+        M._stream_of(Stream, 0)
