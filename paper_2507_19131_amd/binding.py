@@ -472,6 +472,8 @@ def mixaq_scaled_linear_forward(h, x, y, x_scales=None, y_scales=None, workspace
     if workspace is not None:
         if workspace.get_device() != at:
             raise ValueError("workspace must be on the current device (it is on %s)" % workspace.device)
+        if not workspace.is_contiguous():                 # (its bytes would not be those that follow its first)
+            raise ValueError("workspace must be contiguous (strides %s)" % (tuple(workspace.stride()),))
         ws, n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(load().mixaq_scaled_linear_forward(h, a, rows, b, ws, n, _stream_of(stream, at)))
     return y

@@ -114,3 +114,15 @@ def test_a_stream_of_another_device_is_refused(monkeypatch):
     assert M._stream_of(Stream, 1).value == 0x1234
     with pytest.raises(ValueError, match="stream"):
         M._stream_of(Stream, 0)
+
+
+def test_a_workspace_has_the_bytes_it_says(calls):
+    """An expanded tensor counts values that it has no memory for, a transposed or sliced one memory that belongs to others."""
+    x = torch.zeros((5, 8))
+    byte = torch.zeros(1, dtype=torch.uint8)
+    for ws in (byte.expand(1 << 20), torch.zeros((64, 64)).t(), torch.zeros(64)[::2], torch.zeros((8, 8))[:, :4]):
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            M.mixaq_scaled_linear_forward(layer(8, 8), x, torch.zeros((5, 8)), workspace=ws)
+    assert not calls
+    M.mixaq_scaled_linear_forward(layer(8, 8), x, torch.zeros((5, 8)), workspace=torch.zeros((8, 8))[2:])
+    assert calls[0][1][5] == 6 * 8 * 4
