@@ -275,8 +275,8 @@ int mixaq_downsample_forward_taps(const mixaq_downsample *h, const float *x, flo
  * A matrix of rows (tokens), in device memory.  Row r starts at data + r * stride; of a block of 128 columns b (the last one may be
  * shorter) row r's scale is scales[b * scale_stride + r], and the values that codes stand for are code * scale.  Values may
  * start at any multiple of their size and have any stride >= columns.  Codes and their stride are multiples of 16 bytes, and every row
- * (the last one too) has room for its columns rounded up to 16: those bytes are read, what they hold changes nothing, and they are never
- * written.  Calls take 0 .. 2^30 rows; of no rows nothing is read, the pointers included. */
+ * of a layer's x (the last one too) has room for its columns rounded up to 16: those bytes are read, what they hold changes nothing, and
+ * nothing is ever written behind a row's columns.  Calls take 0 .. 2^30 rows; of no rows nothing is read, the pointers included. */
 typedef enum { MIXAQ_F32 = 0, MIXAQ_F16 = 1, MIXAQ_BF16 = 2, MIXAQ_E4M3 = 3 } mixaq_type;
 typedef struct {
     void    *data;

@@ -468,6 +468,8 @@ def mixaq_scaled_linear_forward(h, x, y, x_scales=None, y_scales=None, workspace
         raise ValueError("x %s, y %s do not fit a layer of %d inputs and %d outputs" % (tuple(x.shape), tuple(y.shape), h.K, h.N))
     at = _on_device(x, "x")
     a, b = _rows(x, "x", at, x_scales), _rows(y, "y", at, y_scales)
+    if a.type == 3 and h.K % 16 and rows and x.storage_offset() + (rows - 1) * a.stride + -(-h.K // 16) * 16 > x.untyped_storage().nbytes():
+        raise ValueError("x's last row has no room for its %d codes rounded up to 16 (alloc_codes leaves it)" % h.K)
     ws, n = None, 0
     if workspace is not None:
         if workspace.get_device() != at:

@@ -126,3 +126,19 @@ def test_a_workspace_has_the_bytes_it_says(calls):
     assert not calls
     M.mixaq_scaled_linear_forward(layer(8, 8), x, torch.zeros((5, 8)), workspace=torch.zeros((8, 8))[2:])
     assert calls[0][1][5] == 6 * 8 * 4
+
+
+def test_codes_have_room_for_whole_16_bytes(calls):
+    """A layer reads a row's codes 16 at a time, those of the last row (or the only one, whose stride means nothing) too."""
+    y = torch.zeros((1, 8))
+    byte = lambda n: torch.zeros(n, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    scales = torch.ones((1, 3))
+    for x in (byte(100).view(1, 100), byte(111).view(1, 111)[:, :100], byte(2 * 112 + 100).as_strided((3, 100), (112, 1)), byte(116)[16:].view(1, 100)):
+        with pytest.raises(ValueError, match="room"):
+            M.mixaq_scaled_linear_forward(layer(100, 8), x, y.expand(len(x), 8).contiguous(), x_scales=scales[:, :len(x)])
+    assert not calls
+    for x in (byte(112).view(1, 112)[:, :100], byte(3 * 112).as_strided((3, 100), (112, 1)), byte(128)[16:].view(1, 112)[:, :100], byte(100)[:0].view(0, 100)):
+        M.mixaq_scaled_linear_forward(layer(100, 8), x, y.expand(len(x), 8).contiguous(), x_scales=scales[:, :len(x)])
+    M.mixaq_scaled_linear_forward(layer(96, 8), byte(96).view(1, 96), y, x_scales=scales[:, :1])
+    assert len(calls) == 5
+    M.mixaq_scaled_quantize(torch.zeros((1, 100)), byte(100).view(1, 100), scales[:, :1])      # written without what is behind the columns
