@@ -342,7 +342,7 @@ typedef struct {
 /* x: values.  branch: values, or NULL (y = residual_scale * x; then no post_norm and no gate).  y: values of x's type, or NULL.  out:
  * values, or codes as mixaq_scaled_quantize with block_rows 1 makes them of the binary32 results, or NULL (then no pre_norm); one
  * of y and out is given.  y or out may be x or branch itself (same data, stride and type); apart from that the outputs overlap
- * neither the inputs nor each other.  One kernel, allocates nothing. */
+ * neither the inputs, the vectors among them, nor each other.  One kernel, allocates nothing. */
 int mixaq_residual_norm(const mixaq_residual_norm_desc *desc, const mixaq_residual_norm_params *params, const mixaq_rows *x,
                         const mixaq_rows *branch, const mixaq_rows *y, const mixaq_rows *out, int32_t rows, void *stream);
 

@@ -269,6 +269,13 @@ extern "C" int mixaq_residual_norm(const mixaq_residual_norm_desc* desc, const m
             const Extent e = extent_of(*in, rows, d.C);
             if ((!same_place(*outputs[i], *in) && overlap(o, e)) || overlap(os, e)) return fail(MIXAQ_E_SHAPE, "%s and %s overlap", names[i], in == x ? "x" : "branch");
         }
+        const float* const vectors[5] = {params->post_gamma, params->post_beta, params->pre_gamma, params->pre_beta, params->gate};
+        const char* const of[5] = {"post_gamma", "post_beta", "pre_gamma", "pre_beta", "gate"};
+        for (int v = 0; v < 5; ++v) {
+            const long long count = v < 4 ? 1 : (rows - 1LL) / std::max(d.rows_per_gate, 1) + 1;
+            const Extent e = {(uintptr_t)vectors[v], d.C * 4LL, vectors[v] ? count : 0, d.C * 4LL};
+            if (overlap(o, e) || overlap(os, e)) return fail(MIXAQ_E_SHAPE, "%s and %s overlap", names[i], of[v]);
+        }
         if (overlap(o, os)) return fail(MIXAQ_E_SHAPE, "codes and scales of %s overlap", names[i]);
     }
     if (y && out && (overlap(extent_of(*y, rows, d.C), extent_of(*out, rows, d.C)) || overlap(extent_of(*y, rows, d.C), scales_of(*out, rows, d.C))))

@@ -142,3 +142,30 @@ def test_codes_have_room_for_whole_16_bytes(calls):
     M.mixaq_scaled_linear_forward(layer(96, 8), byte(96).view(1, 96), y, x_scales=scales[:, :1])
     assert len(calls) == 5
     M.mixaq_scaled_quantize(torch.zeros((1, 100)), byte(100).view(1, 100), scales[:, :1])      # written without what is behind the columns
+
+
+# ---------------------------------------------------------------- the library
+def rows(data, stride=256, kind=2, scales=None, scale_stride=0):
+    return M.Rows(data, stride, kind, scales, scale_stride)
+
+
+VECTORS = ("post_gamma", "post_beta", "pre_gamma", "pre_beta", "gate")
+
+
+@pytest.mark.parametrize("vector", VECTORS)
+@pytest.mark.parametrize("written", ["y", "out", "scales"])
+def test_norms_refuse_outputs_over_their_vectors(vector, written):
+    """A vector that a row's results replace would be another one for the next row."""
+    n, channels = 10, 200
+    desc = M.ResidualNormDesc(channels, 1, 2, 3, 1e-5, 1e-5, 1.0)
+    x, f, y, out, scales = (AT + (i << 20) for i in range(5))
+    at = {"y": y, "out": out, "scales": scales}[written]
+    size = {"y": (n - 1) * 512 + 400, "out": (n - 1) * 256 + 200, "scales": 4 * (16 + n)}[written]       # bytes from the first to the last
+    length = 4 * channels * (4 if vector == "gate" else 1)                                              # gates: ceil(10 / 3)
+
+    def call(where):
+        p = M.ResidualNormParams(**{vector: where})
+        return M.load().mixaq_residual_norm(C.byref(desc), C.byref(p), rows(x), rows(f), rows(y), rows(out, 256, 3, scales, 16), n, None)
+
+    for where in (at, at + size - 4, at - length + 4):
+        refused("%s and %s overlap" % ("y" if written == "y" else "out", vector), call(where))
