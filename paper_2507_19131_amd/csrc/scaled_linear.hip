@@ -678,24 +678,35 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void tile_kernel(LinearArgs A, int
     }
 }
 
+// Quantizes x first where it is given as values; behind the checks of the product that follows.
+int quantize_first(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
+{
+    if (!values) return MIXAQ_OK;
+    return launch_quantize(*values, A.M, A.K, 1, {(void*)A.x, A.ldx, MIXAQ_E4M3, (float*)A.sx, A.ldsx}, st);
+}
+
 template <int YT, int MT, int WM, int WN>
-int launch_tiles(const LinearArgs& A, hipStream_t st)
+int launch_tiles(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
 {
     constexpr int TM = 32 * MT * WM;
     const int tiles_m = (int)(((long long)A.M + TM - 1) / TM), tiles_n = (A.NB + WN - 1) / WN;
     const long long blocks = ((long long)tiles_m * tiles_n + 7) / 8 * 8;
     if (blocks * WM * WN * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
+    const int rc = quantize_first(A, values, st);
+    if (rc) return rc;
     hipLaunchKernelGGL((tile_kernel<YT, MT, WM, WN>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, tiles_m, tiles_n, FastDiv(GROUP_M * tiles_n));
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
 }
 
 template <int XT, int YT, int MR, int NR, int NW>
-int launch_split(const LinearArgs& A, hipStream_t st)
+int launch_split(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
 {
     const long long row_tiles = ((long long)A.M + 16 * MR - 1) / (16 * MR), groups = row_tiles * (A.NB * 8 / NR);
     const long long blocks = (groups + 7) / 8 * 8;
     if (blocks * NW * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
+    const int rc = quantize_first(A, values, st);
+    if (rc) return rc;
     hipLaunchKernelGGL((split_kernel<XT, YT, MR, NR, NW>), dim3((unsigned)blocks), dim3(NW * 64), 0, st, A, (int)row_tiles, FastDiv((int)row_tiles), (int)groups);
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
@@ -738,30 +749,30 @@ bool quantized_inside(int M, const mixaq_scaled_linear* h)
 }
 
 template <int XT, int YT>
-int launch_few(const LinearArgs& A, hipStream_t st)
+int launch_few(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
 {
-    if constexpr (YT == MIXAQ_E4M3) return launch_split<XT, YT, 1, 8, 8>(A, st);
-    else return launch_split<XT, YT, 1, 1, 8>(A, st);
+    if constexpr (YT == MIXAQ_E4M3) return launch_split<XT, YT, 1, 8, 8>(A, values, st);
+    else return launch_split<XT, YT, 1, 1, 8>(A, values, st);
 }
 template <int YT>
-int launch_linear(const LinearArgs& A, Form form, int x_type, hipStream_t st)
+int launch_linear(const LinearArgs& A, Form form, int x_type, const mixaq_rows* values, hipStream_t st)
 {
     switch (form) {
     case FORM_FEW:
-        if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT>(A, st);
-        if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT>(A, st);
-        if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT>(A, st);
-        return launch_few<MIXAQ_E4M3, YT>(A, st);
+        if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT>(A, values, st);
+        if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT>(A, values, st);
+        if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT>(A, values, st);
+        return launch_few<MIXAQ_E4M3, YT>(A, values, st);
     case FORM_MID:
-        if constexpr (YT == MIXAQ_E4M3) return launch_split<MIXAQ_E4M3, YT, 1, 8, 8>(A, st);
-        else return launch_split<MIXAQ_E4M3, YT, 2, 2, 8>(A, st);
+        if constexpr (YT == MIXAQ_E4M3) return launch_split<MIXAQ_E4M3, YT, 1, 8, 8>(A, values, st);
+        else return launch_split<MIXAQ_E4M3, YT, 2, 2, 8>(A, values, st);
     case FORM_SPLIT:
-        if constexpr (YT == MIXAQ_E4M3) return launch_split<MIXAQ_E4M3, YT, 2, 8, 4>(A, st);
-        else return launch_split<MIXAQ_E4M3, YT, 4, 4, 4>(A, st);
-    case FORM_TILE: return launch_tiles<YT, 1, 4, 1>(A, st);
+        if constexpr (YT == MIXAQ_E4M3) return launch_split<MIXAQ_E4M3, YT, 2, 8, 4>(A, values, st);
+        else return launch_split<MIXAQ_E4M3, YT, 4, 4, 4>(A, values, st);
+    case FORM_TILE: return launch_tiles<YT, 1, 4, 1>(A, values, st);
     default:
-        if constexpr (exact_sums(YT)) return launch_tiles<YT, 1, 8, 1>(A, st);
-        else return launch_tiles<YT, 2, 4, 2>(A, st);
+        if constexpr (exact_sums(YT)) return launch_tiles<YT, 1, 8, 1>(A, values, st);
+        else return launch_tiles<YT, 2, 4, 2>(A, values, st);
     }
 }
 
@@ -879,17 +890,13 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
     A.M = rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
     A.gelu = h->d.activation == 1;
     const Form form = form_of(rows, h, exact_sums(y->type), A.ldx);
-    int x_type = x->type;
-    if (need) {
-        rc = launch_quantize(*x, rows, K, 1, codes, st);
-        if (rc) return rc;
-        x_type = MIXAQ_E4M3;
-    }
+    const mixaq_rows* const values = need ? x : nullptr;
+    const int x_type = codes.type;
     switch (y->type) {
-    case MIXAQ_F32: return launch_linear<MIXAQ_F32>(A, form, x_type, st);
-    case MIXAQ_F16: return launch_linear<MIXAQ_F16>(A, form, x_type, st);
-    case MIXAQ_BF16: return launch_linear<MIXAQ_BF16>(A, form, x_type, st);
-    default: return launch_linear<MIXAQ_E4M3>(A, form, x_type, st);
+    case MIXAQ_F32: return launch_linear<MIXAQ_F32>(A, form, x_type, values, st);
+    case MIXAQ_F16: return launch_linear<MIXAQ_F16>(A, form, x_type, values, st);
+    case MIXAQ_BF16: return launch_linear<MIXAQ_BF16>(A, form, x_type, values, st);
+    default: return launch_linear<MIXAQ_E4M3>(A, form, x_type, values, st);
     }
 }
 

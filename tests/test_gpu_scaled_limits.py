@@ -24,3 +24,19 @@ def test_a_row_of_nearly_2_31_columns():
         want, s = R.quantize(x[:, at:at + n].float().cpu().numpy())
         assert np.array_equal(codes[:, at:at + n].view(torch.uint8).cpu().numpy(), want)
         assert np.array_equal(scales[at // 128:at // 128 + s.shape[0]].cpu().double().numpy(), s)
+
+
+def test_a_product_of_too_many_tiles_is_refused_before_anything_runs():
+    """Values are not quantized either."""
+    rows, N = 1 << 22, 65536
+    w, s_w = M.alloc_codes(N, 1, 128)
+    s_w.fill_(1.0)
+    h = M.mixaq_scaled_linear_create(w, s_w)
+    x = torch.ones((rows, 1), dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((M.mixaq_scaled_linear_workspace_bytes(h, rows, torch.bfloat16, torch.bfloat16),), 0x5A, dtype=torch.uint8, device="cuda")
+    y = M.Rows(1 << 56, N, 2, None, 0)                     # an address that no call may touch
+    rc = M.load().mixaq_scaled_linear_forward(h, M._rows(x, "x", 0), rows, y, ws.data_ptr(), ws.numel(), None)
+    assert rc == -2 and b"too many" in M.load().mixaq_last_error()
+    torch.cuda.synchronize()
+    M.mixaq_scaled_linear_destroy(h)
+    assert bool((ws == 0x5A).all())
