@@ -295,8 +295,8 @@ int mixaq_scaled_quantize(const mixaq_rows *x, int32_t rows, int32_t columns, in
 
 /* y = act(x w^T + bias): on codes of x [rows, K] and of w [N, K].  Of each block of 128 columns the exact products are summed, then one fused
  * multiply-add with the product of the two scales takes the sum to the others; one rounding to y's type at the end.  Sums are binary32; for
- * a y of 16 bits the sum of a block is that of the 8-bit matrix instruction, which keeps 14 bits of eight neighbouring products, counted
- * from the largest of them.  x may be given as values: they are quantized first, as mixaq_scaled_quantize with block_rows 1 does, with the same
+ * a y in bf16 the sum of a block is that of the 8-bit matrix instruction, which keeps 14 bits of eight neighbouring products, counted
+ * from the largest of them (products that cancel leave an error of up to 7 * 2^-13 of their size; a y in f16 or f32 has exact products).  x may be given as values: they are quantized first, as mixaq_scaled_quantize with block_rows 1 does, with the same
  * result (but codes whose rows lie 4 MB or more apart may be summed in another order).  y may be codes: the binary32 results are
  * quantized, as mixaq_scaled_quantize does. */
 typedef struct {

@@ -179,11 +179,12 @@ __device__ __forceinline__ v4i load_codes(const uint8_t* row, int k, int K)
 
 // ---- products of one block of 128 -----------------------------------------------------------------------------------------
 // The 8-bit instruction sums groups of eight neighbouring products at the exponent of the largest of them and keeps 14 bits of each
-// (measured: of 2^16 + 2^s within a group s = 3 arrives and s = 2 does not; across groups 24 bits do): up to 7 * 2^-13 of a group's largest product,
-// 1.5e-5 of the results' root mean square on normal values, 2.8e-5 with an outlier channel.  That is a hundredth of what rounding to bf16
-// costs and a tenth of f16's, but not binary32: results of 32 bits, and those that become codes, whose scale is kept in 32 bits, are summed
-// by the f16 instruction (e4m3 values are f16 values, their products exact, 1e-8), which takes twice the time.
-constexpr bool exact_sums(int y_type) { return y_type == MIXAQ_F32 || y_type == MIXAQ_E4M3; }
+// (measured: of 2^16 + 2^s within a group s = 3 arrives and s = 2 does not; across groups 24 bits do): up to 7 * 2^-13 of a group's largest product
+// is lost, whatever is left of it when it cancels.  Of normal values that is 2e-5 of the results' root mean square, with a channel 12 times as large as
+// the others 3e-5, 1000 times 1.1e-4: 1, 2 and 7 % of what rounding to bf16 costs, and results in bf16 are summed so.  Of f16's rounding it would be
+// 10, 16 and 50 %; results in f16, those of 32 bits and those that become codes, whose scale is kept in 32 bits, are summed by the f16 instruction
+// (e4m3 values are f16 values, their products exact, 1e-8), which takes twice the time (16384 x 4096 x 3840 480 us, to bf16 230).
+constexpr bool exact_sums(int y_type) { return y_type != MIXAQ_BF16; }
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
@@ -722,7 +723,7 @@ int launch_split(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
 //   SPLIT below 96 tiles of 128 x 128, with more than 32 blocks of K below 192, codes out: 1024 x 1024 x 1024 8.9 / 10.9 (tile)    1024 x 4096 x 1024
 //     21.4 / 39.3    269 x 5504 x 5984 (141 tiles, 43 blocks) 47.7 / 55.4 |  4704 x 1536 x 384 (111 tiles) 21.8 / 17.6    8192 x 256 x 256 (128) 10.6 / 5.7;
 //     bf16 out the same or 5 % to either side at 64
-//   LARGE, 16-bit sums, from 192 tiles of 256 x 256 and two blocks of K: 16384 x 512 x 512 (128) 11.3 (tile) / 13.9    2048 x 1024 x 4096 (128)
+//   LARGE, to bf16, from 192 tiles of 256 x 256 and two blocks of K: 16384 x 512 x 512 (128) 11.3 (tile) / 13.9    2048 x 1024 x 4096 (128)
 //     15.4 / 19.0 |  16384 x 768 x 768 (192) 18.7 / 17.4    8192 x 256 x 2048 (256) 14.2 / 12.8    4096 x 2048 x 4096 (256) 43.9 / 34.9; with a
 //     GELU, which a second workgroup on the CU hides, from six blocks: 16384 x 384 x 1536 28.4 (tile) / 33.8    100000 x 256 x 1024 108 / 115 |
 //     16384 x 1024 x 2048 57.7 / 52.2
