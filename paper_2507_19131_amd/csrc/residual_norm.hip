@@ -27,23 +27,28 @@ struct NormArgs {
     const float *post_gamma, *post_beta, *pre_gamma, *pre_beta, *gate;
 };
 
-// Sum over the G lanes of a row; with more than a wave, through LDS (`part`: twice a float per wave, used in turn, so that one barrier is
-// enough: who writes a half again has passed the barrier of the other one, behind which nobody reads it any more).
-template <int G>
-__device__ __forceinline__ float row_sum(float v, float (*part)[G / 64 + 1], int& turn)
+// Sums over the G lanes of a row, of N values a lane.  With more than a wave, through LDS (`part`: a place per wave, twice, used in turn, so that one
+// barrier is enough: who writes a half again has passed the barrier of the other one, behind which nobody reads it any more): a lane reads one
+// wave's sums, and its neighbours add them up.
+struct Sums { float v[2]; };
+template <int G> using Part = Sums[G < 64 ? 1 : G / 64];
+template <int G, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], Part<G>* part, int& turn)
 {
-    if constexpr (G == 16) return __uint_as_float(over16(__float_as_uint(v), SumOf()));
-    v = __uint_as_float(over64(__float_as_uint(v), SumOf()));
-    if constexpr (G > 64) {
-        float* const p = part[turn];
-        turn ^= 1;
-        if ((threadIdx.x & 63) == 0) p[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < G / 64; w += 4) v += (p[w] + p[w + 1]) + (p[w + 2] + p[w + 3]);
+    for (int n = 0; n < N; ++n) v[n] = __uint_as_float(G == 16 ? over16(__float_as_uint(v[n]), SumOf()) : over64(__float_as_uint(v[n]), SumOf()));
+    if constexpr (G > 64) {
+        Sums* const p = part[turn];
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) p[threadIdx.x >> 6].v[n] = v[n];
+        }
+        __syncthreads();
+        const Sums& mine = p[threadIdx.x % (G / 64)];
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = __uint_as_float(over_few<G / 64>(__float_as_uint(mine.v[n]), SumOf()));
     }
-    return v;
 }
 
 // A vector of parameters: a lane's values of it.
@@ -60,50 +65,68 @@ __device__ __forceinline__ void load_vector(Vector<V>& to, const float* from, co
     }
 }
 
-// One norm of a row whose values lie in registers, V times eight a lane: mean first, then the squares of what is left, so that
-// a large mean costs no digits.  Sums in binary32.
+// One norm of a row whose values lie in registers, V times eight a lane: mean first, then the squares of what is left.  Beside the squares what is left
+// is summed as well: that is what the roundings of the first sum have kept out of the mean (of equal values of 1000 up to 2e-3, which 1 / sqrt(eps)
+// made 0.6 instead of 0), and it comes off the mean square and the values.  So a large mean costs no digits but the values' own.  An addition a value and a
+// second value in the exchange: us of two LayerNorms, without it / with it, 68208 x 96 of f32 to codes 19.2 / 19.5, of bf16 14.4 / 15.6, 17000 x 768 28.1 / 29.2,
+// 8190 x 4096 58.0 / 59.6.  Sums in binary32.
 template <int G, int V, bool TINY>
 __device__ __forceinline__ void norm_row(float (&v)[V][8], int kind, float eps, const Vector<V>& gamma, const Vector<V>& beta, const Eight (&c)[V],
-                                         const NormArgs& A, float (*part)[G / 64 + 1], int& turn)
+                                         const NormArgs& A, Part<G>* part, int& turn)
 {
     float mean = 0.0f;
     if (kind == NORM_LAYER) {
-        float s = 0.0f;
+        float s[1] = {0.0f};
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += own8<TINY>(c[j], e, A.C) ? v[j][e] : 0.0f;
-        mean = row_sum<G>(s, part, turn) * A.inv_C;
+            for (int e = 0; e < 8; ++e) s[0] += own8<TINY>(c[j], e, A.C) ? v[j][e] : 0.0f;
+        row_sums<G>(s, part, turn);
+        mean = s[0] * A.inv_C;
     }
-    float q = 0.0f;
+    float q[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             v[j][e] -= mean;
             const float o = own8<TINY>(c[j], e, A.C) ? v[j][e] : 0.0f;
-            q = fmaf(o, o, q);
+            q[0] += o;
+            q[1] = fmaf(o, o, q[1]);
         }
-    const float r = 1.0f / sqrtf(row_sum<G>(q, part, turn) * A.inv_C + eps);
+    // An RMS norm has no use for q[0], but an exchange of its own costs registers, which rows of more than a wave and of two times eight values a lane lack:
+    // 2000 x 16384 95 us with it, 89 without (8190 x 4096 of RMS norms, which have them, 55 and 57).
+    if (kind == NORM_LAYER || (V == 2 && G != 256)) {
+        row_sums<G>(q, part, turn);
+    } else {
+        float only[1] = {q[1]};
+        row_sums<G>(only, part, turn);
+        q[1] = only[0];
+    }
+    const float rest = kind == NORM_LAYER ? q[0] * A.inv_C : 0.0f;
+    float square = fmaf(-rest, rest, q[1] * A.inv_C);
+    square = square < 0.0f ? 0.0f : square;                           // (a NaN stays one)
+    const float r = 1.0f / sqrtf(square + eps), off = -rest * r;
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[j][e] = fmaf(v[j][e] * r, gamma.v[j][e], beta.v[j][e]);
+        for (int e = 0; e < 8; ++e) v[j][e] = fmaf(fmaf(v[j][e], r, off), gamma.v[j][e], beta.v[j][e]);
 }
 
 // A workgroup's next row is on its way while this one is worked on: with about three workgroups a CU, whose rows would otherwise be
-// requested, reduced and stored in turn, memory is seldom without requests.  KEEP: the vectors of both norms and the gate stay in registers
+// requested, reduced and stored in turn, memory is seldom without requests (of 16-bit values three waves a SIMD are asked for, which 129 to 256 and 513 to
+// 1024 columns would miss by few registers: 17000 x 768 29 us instead of 39).  KEEP: the vectors of both norms and the gate stay in registers
 // from row to row; else they come anew (from the caches) for every row, where four of them would not fit beside it.
 // What bounds it is memory: 8190 x 4096 of bf16 with two outputs 4.4 TB/s, a copy of that size 5.1.  Rows that start anywhere (an
 // odd width) cost a third more: every vector access of a wave then touches a line more.
 template <int TX, int TB, int G, int V, bool TINY>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormArgs A)
+__global__ __launch_bounds__(G < 256 ? 256 : G, G <= 256 && sizeof(typename TypeOf<TX>::T) + sizeof(typename TypeOf<TB>::T) == 4 ? 3 : 1) void residual_norm_kernel(NormArgs A)
 {
     using X = typename TypeOf<TX>::T;
     using B = typename TypeOf<TB>::T;
     constexpr bool KEEP = G <= 256 || V == 1;
     constexpr int ROWS = G < 256 ? 256 / G : 1;                       // at one time
-    __shared__ float part[2][G / 64 + 1];
+    __shared__ Part<G> part[2];
     int turn = 0;
     const int l = threadIdx.x % G;
     Eight c[V];

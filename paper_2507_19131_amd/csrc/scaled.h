@@ -117,14 +117,18 @@ __device__ __forceinline__ void store_codes8(uint8_t* row, Eight c, int C, const
 
 // ---- exchanges between lanes, all in the vector unit ------------------------------------------------------------
 template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
-template <typename Op>
-__device__ __forceinline__ unsigned over16(unsigned v, Op op)         // of 16 lanes
+template <int LANES, typename Op>
+__device__ __forceinline__ unsigned over_few(unsigned v, Op op)       // of 4 or 16 neighbouring lanes
 {
+    static_assert(LANES == 4 || LANES == 16, "");
     v = op(v, dpp<0xB1>(v));                                          // neighbours
     v = op(v, dpp<0x4E>(v));                                          // pairs
+    if constexpr (LANES == 4) return v;
     v = op(v, dpp<0x141>(v));                                         // quads, by the mirror of eight lanes
     return op(v, dpp<0x140>(v));                                      // eights, by the mirror of 16
 }
+template <typename Op>
+__device__ __forceinline__ unsigned over16(unsigned v, Op op) { return over_few<16>(v, op); }
 template <typename Op>
 __device__ __forceinline__ unsigned over4rows(unsigned v, Op op)      // of the four lanes l, l + 16, l + 32, l + 48
 {
