@@ -1,6 +1,7 @@
 // Linear layers on 8-bit float codes with a scale per 128 columns: y = act(x w^T + bias), the products on the e4m3 matrix
 // instruction of gfx950, 128 deep, which is one block of scales.
 #include "scaled.h"
+#include "scaled_forms.h"
 
 #include <algorithm>
 #include <cmath>
@@ -713,42 +714,6 @@ int launch_split(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
     return MIXAQ_OK;
 }
 
-// Which kernel takes a product: by rows, the layer and how sums are taken, never by x's type or by whether exact sums become codes, so that values
-// in and codes out are the same results.  us (graph replays; few / split, or as it says):
-//   FEW while its workgroups - 16 rows and 16 outputs each - times their blocks of K stay few, and for up to 16 rows:
-//     64 x 1024 x 1024 3.2 / 7.1    128 x 4096 x 1024 7.2 / 16.8    256 x 1024 x 1024 4.9 / 7.2    1001 x 1000 x 333 5.8 / 7.2 |  1024 x 1024 x 1024
-//     13.2 / 8.0    512 x 2048 x 2048 22.9 / 11.5    256 x 4096 x 4096 39.5 / 19.1
-//   MID, 32 x 32 by eight waves, where SPLIT's 64 x 64 would be fewer than 192 (few / mid / split): 64 x 4096 x 4096 12.1 / 7.8 / 16.9    682 x 3584 x 352
-//     13.2 / 11.5 / 17.2    3272 x 7840 x 32 30.5 / 20.4 / 31.0 |  2048 x 1536 x 384 (192) 11.1 (mid) / 10.6    512 x 2048 x 2048 (256) 13.4 / 11.4
-//   SPLIT below 96 tiles of 128 x 128, with more than 32 blocks of K below 192, codes out: 1024 x 1024 x 1024 8.9 / 10.9 (tile)    1024 x 4096 x 1024
-//     21.4 / 39.3    269 x 5504 x 5984 (141 tiles, 43 blocks) 47.7 / 55.4 |  4704 x 1536 x 384 (111 tiles) 21.8 / 17.6    8192 x 256 x 256 (128) 10.6 / 5.7;
-//     bf16 out the same or 5 % to either side at 64
-//   LARGE, to bf16, from 192 tiles of 256 x 256 and two blocks of K: 16384 x 512 x 512 (128) 11.3 (tile) / 13.9    2048 x 1024 x 4096 (128)
-//     15.4 / 19.0 |  16384 x 768 x 768 (192) 18.7 / 17.4    8192 x 256 x 2048 (256) 14.2 / 12.8    4096 x 2048 x 4096 (256) 43.9 / 34.9; with a
-//     GELU, which a second workgroup on the CU hides, from six blocks: 16384 x 384 x 1536 28.4 (tile) / 33.8    100000 x 256 x 1024 108 / 115 |
-//     16384 x 1024 x 2048 57.7 / 52.2
-//   LARGE, exact sums, from 224 tiles of 256 x 128 and three blocks: 4096 x 4096 x 1024 (128) 42.6 (tile) / 50.9    65536 x 256 x 1024 (two blocks)
-//     56.1 / 60.8 |  4704 x 384 x 1536 (228) 10.8 / 10.4    8192 x 1024 x 1024 (256) 22.4 / 19.7    16384 x 1024 x 2048 75.3 / 70.2
-enum Form { FORM_FEW, FORM_MID, FORM_SPLIT, FORM_TILE, FORM_LARGE };
-Form form_of(int M, const mixaq_scaled_linear* h, bool exact, long long ldx)
-{
-    const long long tiles16 = (M + 15LL) / 16 * h->NB * 8, tiles128 = (M + 127LL) / 128 * h->NB;
-    const long long large = (M + 255LL) / 256 * (exact ? h->NB : (h->NB + 1) / 2);
-    if (M <= 16 || tiles16 * h->KB <= std::min(16384, 5000 + 1400 * h->KB)) return FORM_FEW;
-    if ((M + 63LL) / 64 * h->NB * 2 < 192) return FORM_MID;
-    if (tiles128 < (h->KB > 32 ? 192 : 96) || ldx >= (1 << 22)) return FORM_SPLIT;      // (rows 4 MB apart: the tiles count in 32 bits)
-    return large >= (exact ? 224 : 192) && h->KB >= (exact ? 3 : h->d.activation ? 6 : 2) ? FORM_LARGE : FORM_TILE;
-}
-
-// Whether values are quantized on their way into FEW's product: every workgroup does it for its 16 rows, so with many workgroups or blocks a launch of
-// its own is shorter.  us of the GPU, f32 / bf16 values, in one launch and in two (the second takes the host another 3.5):
-//     1 x 1024 x 4096 3.3 / 3.5, 4.8    64 x 1024 x 1024 4.7 / 4.1, 6.0    1 x 4096 x 4096 6.1 / 6.8, 6.1    256 x 1024 x 1024 10.5 / 7.8, 7.9 |
-//     16 x 8192 x 1024 17 / 11, 10    1001 x 1000 x 333 21 / 13, 11    64 x 4096 x 4096 33 / 21, 15
-bool quantized_inside(int M, const mixaq_scaled_linear* h)
-{
-    return form_of(M, h, true, 0) == FORM_FEW && h->KB <= 32 && (M + 15LL) / 16 * h->NB * 8 * h->KB <= 8192;       // (FEW whatever the sums)
-}
-
 template <int XT, int YT>
 int launch_few(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
 {
@@ -756,21 +721,21 @@ int launch_few(const LinearArgs& A, const mixaq_rows* values, hipStream_t st)
     else return launch_split<XT, YT, 1, 1, 8>(A, values, st);
 }
 template <int YT>
-int launch_linear(const LinearArgs& A, Form form, int x_type, const mixaq_rows* values, hipStream_t st)
+int launch_linear(const LinearArgs& A, ScaledForm form, int x_type, const mixaq_rows* values, hipStream_t st)
 {
     switch (form) {
-    case FORM_FEW:
+    case SCALED_FEW:
         if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT>(A, values, st);
         if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT>(A, values, st);
         if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT>(A, values, st);
         return launch_few<MIXAQ_E4M3, YT>(A, values, st);
-    case FORM_MID:
+    case SCALED_MID:
         if constexpr (YT == MIXAQ_E4M3) return launch_split<MIXAQ_E4M3, YT, 1, 8, 8>(A, values, st);
         else return launch_split<MIXAQ_E4M3, YT, 2, 2, 8>(A, values, st);
-    case FORM_SPLIT:
+    case SCALED_SPLIT:
         if constexpr (YT == MIXAQ_E4M3) return launch_split<MIXAQ_E4M3, YT, 2, 8, 4>(A, values, st);
         else return launch_split<MIXAQ_E4M3, YT, 4, 4, 4>(A, values, st);
-    case FORM_TILE: return launch_tiles<YT, 1, 4, 1>(A, values, st);
+    case SCALED_TILE: return launch_tiles<YT, 1, 4, 1>(A, values, st);
     default:
         if constexpr (exact_sums(YT)) return launch_tiles<YT, 1, 8, 1>(A, values, st);
         else return launch_tiles<YT, 2, 4, 2>(A, values, st);
@@ -783,7 +748,7 @@ size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 // the workspace: codes and scales of x, where it is given as values and not quantized on its way into the product
 size_t workspace_of(const mixaq_scaled_linear* h, int32_t rows, int32_t x_type)
 {
-    if (x_type == MIXAQ_E4M3 || rows == 0 || quantized_inside(rows, h)) return 0;
+    if (x_type == MIXAQ_E4M3 || rows == 0 || quantized_inside(rows, h->KB, h->NB)) return 0;
     return align256((size_t)rows * round_up16(h->d.K)) + align256((size_t)rows * h->KB * 4);
 }
 
@@ -890,7 +855,7 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear* h, const mixaq_rows* 
     A.sy = y->scales; A.ldsy = y->scale_stride;
     A.M = rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
     A.gelu = h->d.activation == 1;
-    const Form form = form_of(rows, h, exact_sums(y->type), A.ldx);
+    const ScaledForm form = scaled_form(rows, h->KB, h->NB, A.gelu, exact_sums(y->type), A.ldx);
     const mixaq_rows* const values = need ? x : nullptr;
     const int x_type = codes.type;
     switch (y->type) {

@@ -44,7 +44,7 @@ def cancelling(rows, K, N):
 
 
 # few rows; 32 x 32; 64 x 64; tiles of 128 x 128; large tiles
-SIZES = [(1, 1024, 512), (40, 1000, 333), (300, 504, 1100), (2000, 256, 640), (3000, 128, 512), (8200, 400, 1500)]
+SIZES = [(1, 1024, 512), (40, 1000, 333), (700, 1504, 700), (2000, 256, 640), (6000, 128, 512), (8200, 400, 1500)]
 
 
 @pytest.mark.parametrize("rows,K,N", SIZES)
