@@ -126,3 +126,27 @@ def test_the_deepest_products(rows, K, N, kind):
     p = Product(rows, K, N, False, 3, rows)
     p.check(kind, 2048)
     p.close()
+
+
+@pytest.mark.parametrize("rows", [2000, 300000])
+def test_gelu_of_any_value(rows):
+    """One code of 1 times one weight of 1, scaled by any number: the activation alone, in the kernel of few rows and in a tile."""
+    far = torch.tensor([0.0, -0.0, 1e-45, -1e-45, 2e-38, -2e-38, 1e-20, -1e-20, 7.0, -7.0, 13.0, -13.0, 40.0, -40.0, 1e19, -1e19, 2e19, -2e19, 3.4e38, -3.4e38])
+    v = torch.cat([far, torch.linspace(-14.0, 14.0, rows - len(far))]).cuda()
+    codes, _ = M.alloc_codes(rows, 1)
+    codes.view(torch.uint8).fill_(0x38)
+    w, s_w = M.alloc_codes(16, 1, 128)
+    w.view(torch.uint8).fill_(0x38)
+    s_w.fill_(1.0)
+    h = M.mixaq_scaled_linear_create(w, s_w, None, "gelu")
+    y = torch.empty((rows, 16), device="cuda")
+    M.mixaq_scaled_linear_forward(h, codes, y, x_scales=v[None])
+    assert bool((y == y[:, :1]).all())
+    want = gelu(v.double())
+    want = torch.where(v > 40, v.double(), want)             # (0.5 times them passes no border)
+    off = (y[:, 0].double() - want).abs() - gelu_bound(v.double().clamp(-1e3, 1e3), want) - R.HALF_STEP["f32"] * want.abs()
+    assert float(off.max()) <= 0.0, float(v[off.argmax()])
+    v[0], v[1], v[2] = float("inf"), float("-inf"), float("nan")
+    M.mixaq_scaled_linear_forward(h, codes, y, x_scales=v[None])
+    M.mixaq_scaled_linear_destroy(h)
+    assert bool((y[0] == float("inf")).all()) and bool((y[1] == 0).all()) and bool(y[2].isnan().all())

@@ -69,3 +69,28 @@ def test_the_sizes_compared_with_the_reference_reach_every_kernel(kind, gelu):
 def test_the_sizes_that_tell_exact_sums_from_others_reach_every_kernel(kind):
     from test_gpu_scaled_sums import SIZES
     assert {S.form(*size, kind) for size in SIZES} == set(S.NAMES)
+
+
+def test_the_bound_of_gelu_sees_small_mistakes():
+    """What the bound must not let through: a tail that is cut off, erf from a three-term approximation, one coefficient's last digits."""
+    import torch
+    from test_gpu_scaled_forms import gelu, gelu_bound
+    v = torch.linspace(-8.0, 8.0, 200001, dtype=torch.float64)
+    want = gelu(v)
+    bound = gelu_bound(v, want) + 2.0 ** -24 * want.abs()
+    cut = torch.where(v < -4.2, torch.zeros_like(v), want)
+    z = v.abs() * 0.5 ** 0.5
+    t = 1.0 / (1.0 + 0.47047 * z)
+    erf = 1.0 - (0.3480242 * t - 0.0958798 * t ** 2 + 0.7478556 * t ** 3) * torch.exp(-z * z)
+    few = 0.5 * v * (1.0 + erf * torch.sign(v))
+
+    def fit(first):                                       # the kernel's form, evaluated exactly
+        u, p = v * v, 0.0
+        for c in ("0x1.67ab6cp-28", "-0x1.9e7b64p-22", "0x1.80c28cp-17", "-0x1.4e76fep-13", "-0x1.8fb242p-14", "0x1.ad6ad0p-4"):
+            p = p * u + float.fromhex(c)
+        return v / (1.0 + torch.exp2(-v * (p * u + first)))
+
+    first = float.fromhex("0x1.26aebcp+1")
+    for wrong in (cut, few, fit(first * (1 + 2e-6))):
+        assert bool(((wrong - want).abs() > bound).any())
+    assert bool(((fit(first) - want).abs() <= bound).all())
