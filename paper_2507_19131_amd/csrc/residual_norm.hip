@@ -9,12 +9,6 @@ using namespace mixaq;
 
 namespace {
 
-#define HIP_TRY(expr)                                                                                   \
-    do {                                                                                                \
-        hipError_t e_ = (expr);                                                                         \
-        if (e_ != hipSuccess) return fail(MIXAQ_E_HIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
-
 enum { NORM_NONE = 0, NORM_LAYER = 1, NORM_RMS = 2 };
 
 struct NormArgs {

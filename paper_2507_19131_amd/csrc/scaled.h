@@ -144,6 +144,16 @@ struct SumOf { __device__ unsigned operator()(unsigned a, unsigned b) const { re
 __device__ __forceinline__ unsigned max16(unsigned m) { return over16(m, MaxOf()); }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
+// A call that fails (a creation without memory) leaves its error with the runtime, where the caller's next launch would find it.
+#define HIP_TRY(expr)                                                                                        \
+    do {                                                                                                     \
+        hipError_t e_ = (expr);                                                                              \
+        if (e_ != hipSuccess) {                                                                              \
+            (void)hipGetLastError();                                                                         \
+            return fail(MIXAQ_E_HIP, "%s failed: %s", #expr, hipGetErrorString(e_));                         \
+        }                                                                                                    \
+    } while (0)
+
 constexpr long long MOST_THREADS = 1LL << 32;      // of one launch
 
 inline int size_of(int type) { return type == MIXAQ_F32 ? 4 : type == MIXAQ_E4M3 ? 1 : 2; }

@@ -22,12 +22,6 @@ struct mixaq_scaled_linear {
 
 namespace {
 
-#define HIP_TRY(expr)                                                                                   \
-    do {                                                                                                \
-        hipError_t e_ = (expr);                                                                         \
-        if (e_ != hipSuccess) return fail(MIXAQ_E_HIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
-
 struct LinearArgs {
     const uint8_t* x;                 // codes (split_kernel: or values)
     const float* sx;

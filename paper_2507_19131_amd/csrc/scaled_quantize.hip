@@ -7,12 +7,6 @@ using namespace mixaq;
 
 namespace mixaq {
 
-#define HIP_TRY(expr)                                                                                   \
-    do {                                                                                                \
-        hipError_t e_ = (expr);                                                                         \
-        if (e_ != hipSuccess) return fail(MIXAQ_E_HIP, "%s failed: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
-
 int check_rows(const mixaq_rows* m, const char* name, int32_t columns, bool codes_allowed, int32_t scale_rows)
 {
     if (!m || !m->data) return fail(MIXAQ_E_NULL, "%s is NULL", name);

@@ -40,3 +40,23 @@ def test_a_product_of_too_many_tiles_is_refused_before_anything_runs():
     torch.cuda.synchronize()
     M.mixaq_scaled_linear_destroy(h)
     assert bool((ws == 0x5A).all())
+
+
+def test_a_layer_that_finds_no_memory_leaves_no_error_behind():
+    """The refusal is the creation's own: the calls after it are not taken for failed ones."""
+    n = 65536                                              # 4.3 GB of codes
+    w, s_w = M.alloc_codes(n, n, 128)
+    s_w.fill_(1.0)
+    free, _ = torch.cuda.mem_get_info()
+    rest = torch.empty(free - (2 << 30), dtype=torch.uint8, device="cuda")
+    with pytest.raises(M.MixaqError) as e:
+        M.mixaq_scaled_linear_create(w, s_w)
+    assert e.value.code == -5 and "hipMalloc" in str(e.value)
+    x = torch.ones((3, 8), device="cuda")
+    codes, scales = M.alloc_codes(3, 8)
+    M.mixaq_scaled_quantize(x, codes, scales)
+    M.mixaq_residual_norm(M.make_residual_norm(8), x, out=torch.empty_like(x))
+    torch.cuda.synchronize()
+    assert bool((codes.view(torch.uint8) == 0x7E).all())
+    del rest, w, s_w
+    torch.cuda.empty_cache()
