@@ -296,12 +296,14 @@ int mixaq_scaled_quantize(const mixaq_rows *x, int32_t rows, int32_t columns, in
 /* y = act(x w^T + bias): on codes of x [rows, K] and of w [N, K].  Of each block of 128 columns the exact products are summed, then one fused
  * multiply-add with the product of the two scales takes the sum to the others; one rounding to y's type at the end.  Sums are binary32; for
  * a y in bf16 the sum of a block is that of the 8-bit matrix instruction, which keeps 14 bits of eight neighbouring products, counted
- * from the largest of them (products that cancel leave an error of up to 7 * 2^-13 of their size; a y in f16 or f32 has exact products).  x may be given as values: they are quantized first, as mixaq_scaled_quantize with block_rows 1 does, with the same
- * result (but codes whose rows lie 4 MB or more apart may be summed in another order).  y may be codes: the binary32 results are
- * quantized, as mixaq_scaled_quantize does. */
+ * from the largest of them (products that cancel leave an error of up to 7 * 2^-13 of their size; ask for f16 or f32 where that matters).
+ * x may be given as values: they are quantized first, as mixaq_scaled_quantize with block_rows 1 does, with the same result (but codes
+ * whose rows lie 4 MB or more apart may be summed in another order).  y may be codes: the binary32 results are quantized, as
+ * mixaq_scaled_quantize does.  A kernel is chosen by the number of rows, and kernels add in different orders: the bits of a row's result
+ * may depend on how many rows come with it, and on nothing else of them. */
 typedef struct {
     int32_t K, N;             /* inputs and outputs per row: 1 .. 65536                           */
-    int32_t activation;       /* 0: none, 1: GELU (erf form)                                      */
+    int32_t activation;       /* 0: none, 1: GELU (erf form, to within 2.1e-7 of its argument)    */
 } mixaq_scaled_linear_desc;
 typedef struct {
     mixaq_rows   w;           /* MIXAQ_E4M3, [N][K], scales as of mixaq_scaled_quantize with block_rows 128 */
@@ -327,7 +329,7 @@ int mixaq_scaled_linear_forward(const mixaq_scaled_linear *h, const mixaq_rows *
  *   out = pre_norm(y)
  * in binary32; out takes y before y is rounded to its type.  A norm is 0: none, 1: LayerNorm (biased variance), 2: RMS norm, with
  * gamma (NULL: 1) and beta (NULL: 0).  gate: one vector for every rows_per_gate rows, [ceil(rows / rows_per_gate)][C] (a vector
- * per channel: rows_per_gate >= rows; per image: its rows), NULL: 1.  All vectors: device float. */
+ * per channel: rows_per_gate >= rows; per image: its rows), NULL: 1.  All vectors: device float.  All memory is the current device's. */
 typedef struct {
     int32_t C;                        /* values per row: 1 .. 16384                               */
     int32_t post_norm, pre_norm;      /* 0, 1, 2                                                  */

@@ -210,8 +210,8 @@ __device__ __forceinline__ v4f product(v4i w0, v4i w1, v4i x0, v4i x1)
 // in the order of the waves.  For products of few tiles: a lone row at K = 1024 is one round trip to memory.  A block's scale meets
 // its product where both are of one row, so x may be given as values: a lane holds 32 of the 128 values of its row, the other three
 // lanes of the row the rest, and what it needs as operand is the codes of its own.  What bounds it: a launch and two round trips (1 x 1024 x 4096
-// 2.7 us from codes, 3.4 from values; 4.2 MB of weights would take 0.8), with more rows the operands' way through the caches, each workgroup for
-// itself (64 x 4096 x 4096 11.4 us: 67 MB of weights and as much of x, 12 TB/s).
+// 2.7 us from codes, 3.7 from values; 4.2 MB of weights would take 0.8), with more rows the operands' way through the caches, each workgroup for
+// itself (64 x 4096 x 4096 in 32 x 32 7.9 us: 34 MB of weights and as much of x, 8.5 TB/s; 1001 x 1000 x 333 in 16 x 16 6.0 us: 24 and 21 MB).
 template <int XT>
 __device__ __forceinline__ void operand_of(const LinearArgs& A, int row, int kb, int g, v4i (&x)[2], float& scale)
 {
