@@ -277,12 +277,12 @@ int mixaq_downsample_forward_taps(const mixaq_downsample *h, const float *x, flo
  * start at any multiple of their size and have any stride >= columns.  Codes and their stride are multiples of 16 bytes, and every row
  * of a layer's x (the last one too) has room for its columns rounded up to 16: those bytes are read, what they hold changes nothing, and
  * nothing is ever written behind a row's columns.  Calls take 0 .. 2^30 rows; of no rows nothing is read, the pointers included. */
-typedef enum { MIXAQ_F32 = 0, MIXAQ_F16 = 1, MIXAQ_BF16 = 2, MIXAQ_E4M3 = 3 } mixaq_type;
+typedef enum { MIXAQ_F32 = 0, MIXAQ_F16 = 1, MIXAQ_BF16 = 2, MIXAQ_E4M3 = 3, MIXAQ_I8 = 4 /* the token calls below only */ } mixaq_type;
 typedef struct {
     void    *data;
     int64_t  stride;          /* elements from one row to the next                                 */
     int32_t  type;            /* mixaq_type                                                        */
-    float   *scales;          /* MIXAQ_E4M3 only                                                   */
+    float   *scales;          /* MIXAQ_E4M3, MIXAQ_I8                                              */
     int64_t  scale_stride;    /* MIXAQ_E4M3 only: floats from one block of columns to the next     */
 } mixaq_rows;
 
@@ -347,6 +347,70 @@ typedef struct {
  * neither the inputs, the vectors among them, nor each other.  One kernel, allocates nothing. */
 int mixaq_residual_norm(const mixaq_residual_norm_desc *desc, const mixaq_residual_norm_params *params, const mixaq_rows *x,
                         const mixaq_rows *branch, const mixaq_rows *y, const mixaq_rows *out, int32_t rows, void *stream);
+
+/* ---- linear layers on 8-bit integers with a scale per token, and the group norm of a map ------- */
+
+/* The same layers on int8 codes with one scale for a whole row: of activations a token's, of weights a channel's.  Sums are integers and exact at the
+ * matrix cores' full rate, so a row's bits depend on nothing but the row: not on how many rows come with it, nor on how a call is cut.
+ * Codes are mixaq_rows of type MIXAQ_I8: row r's scale is scales[r] (scale_stride is not read), the values are code * scale; data and stride are
+ * multiples of 16 bytes and every row of a layer's x has room for its columns rounded up to 16, as e4m3 codes have. */
+
+/* Values to codes, of every row:  scale = max(largest |v|, 2^-100) / 127,  code = nearest integer (ties to even) of v * (1/scale),
+ * quotient, inverse and product rounded to binary32.  A row that holds a NaN or an infinity gets the scale NaN and codes 0.  x: values;
+ * q: codes; they must not overlap.  rows may be 0. */
+int mixaq_token_quantize(const mixaq_rows *x, int32_t rows, int32_t columns, const mixaq_rows *q, void *stream);
+
+/* y = act(x w^T + bias) on codes of x [rows, K] and of w [N, K]: act(fma(sum_k c_x c_w, s_x s_w, bias)) in binary32, the sum exact, one rounding to
+ * y's type at the end.  x may be given as values: they are quantized first, as mixaq_token_quantize does, with the same result.  y: values.
+ * With `experts` above 1 the layer holds as many matrices and biases, [experts * N] rows one behind the other, and only
+ * mixaq_token_linear_forward_grouped takes it. */
+typedef struct {
+    int32_t K, N;             /* inputs and outputs per row: 1 .. 65536                           */
+    int32_t experts;          /* 1 .. 4096, experts * N at most 2^24                              */
+    int32_t activation;       /* 0: none, 1: GELU (erf form, to within 2.1e-7 of its argument), 2: SiLU (to within 4e-7 of its argument), 3: ReLU */
+} mixaq_token_linear_desc;
+typedef struct {
+    mixaq_rows   w;           /* MIXAQ_I8, [experts * N][K]                                       */
+    const float *bias;        /* device [experts * N] or NULL                                     */
+} mixaq_token_linear_params;
+typedef struct mixaq_token_linear mixaq_token_linear;
+
+/* Packs the parameters into library-owned device memory in the order that the matrix instruction takes them; the caller's
+ * buffers may be released afterwards.  Synchronises `stream` once before returning. */
+int mixaq_token_linear_create(const mixaq_token_linear_desc *desc, const mixaq_token_linear_params *params, void *stream, mixaq_token_linear **out);
+int mixaq_token_linear_destroy(mixaq_token_linear *h);
+/* Bytes of device workspace that the calls below need for an x of up to `x_rows` rows of this type (0: none, workspace may be NULL); a
+ * workspace is 256-byte aligned.  Calls that may overlap in time need workspaces of their own, captured ones included. */
+int mixaq_token_linear_workspace_bytes(const mixaq_token_linear *h, int32_t x_rows, int32_t x_type, size_t *bytes);
+/* Allocates nothing and does not wait; may be captured.  The memory of x, y and workspace must not overlap.  The handle is not
+ * changed: calls on any streams of its device, which has to be current, may share it. */
+int mixaq_token_linear_forward(const mixaq_token_linear *h, const mixaq_rows *x, int32_t rows, const mixaq_rows *y, void *workspace,
+                               size_t workspace_bytes, void *stream);
+/* Rows sorted by expert:  y[r] = row_weights[r] * act(x[gather[r]] w_e^T + bias_e)  for offsets[e] <= r < offsets[e + 1], e = 0 .. experts - 1.
+ * offsets: device int32 [experts + 1], rising, read by the kernels and never by the host: rows may be shared out anew in a captured graph.  What
+ * lies outside 0 .. rows is cut off; falling offsets leave the rows between them undefined.  gather: device int32 [rows], the row of x that
+ * row r reads, or NULL (row r; then x_rows >= rows); a row whose index lies outside 0 .. x_rows - 1 is left as it was, and so are rows of y
+ * outside offsets[0] .. offsets[experts] - 1.  row_weights: device float [rows] or NULL (1).  x has x_rows rows and is quantized once a row, however often
+ * gather names it.  rows: of y; the list and the weights are as long.  y must overlap none of the other arguments. */
+int mixaq_token_linear_forward_grouped(const mixaq_token_linear *h, const mixaq_rows *x, int32_t x_rows, const int32_t *offsets, const int32_t *gather,
+                                       const float *row_weights, const mixaq_rows *y, int32_t rows, void *workspace, size_t workspace_bytes, void *stream);
+
+/* y = act((x - mean) / sqrt(variance + eps) * gamma + beta) on a batch of channels-last maps: x [images * rows_per_image, C] as the blocks and
+ * layers here leave them, the mean and the (biased) variance those of the C / groups neighbouring channels of all rows of an image.  Sums are taken in
+ * binary64, the rest in binary32.  gamma, beta: device float [C] or NULL (1, 0).  A group that holds a NaN or an infinity becomes NaN. */
+typedef struct {
+    int32_t C, groups;        /* 1 .. 8192 channels; groups: at most 1024, a divisor of C         */
+    int32_t rows_per_image;   /* 1 .. 2^30                                                        */
+    int32_t activation;       /* as of mixaq_token_linear_desc                                    */
+    float   eps;              /* > 0                                                              */
+} mixaq_group_norm_desc;
+typedef struct { const float *gamma, *beta; } mixaq_group_norm_params;
+int mixaq_group_norm_workspace_bytes(const mixaq_group_norm_desc *desc, int32_t rows, size_t *bytes);
+/* x: values.  y: values, or codes as mixaq_token_quantize makes them of the binary32 results.  rows: a multiple of rows_per_image, or 0.  y may be x itself
+ * (same data, stride and type); apart from that the memory of y and of the workspace overlaps no other argument.  Allocates nothing and does not
+ * wait; may be captured; calls that may overlap in time need workspaces of their own. */
+int mixaq_group_norm(const mixaq_group_norm_desc *desc, const mixaq_group_norm_params *params, const mixaq_rows *x, const mixaq_rows *y, int32_t rows,
+                     void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- host-only helpers (no GPU work) ------------------------------------------------------- */
 

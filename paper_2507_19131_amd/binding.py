@@ -81,8 +81,26 @@ class ResidualNormParams(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("post_gamma", "post_beta", "pre_gamma", "pre_beta", "gate")]
 
 
+class TokenLinearDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("K", "N", "experts", "activation")]
+
+
+class TokenLinearParams(C.Structure):
+    _fields_ = [("w", Rows), ("bias", C.c_void_p)]
+
+
+class GroupNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("C", "groups", "rows_per_image", "activation")] + [("eps", C.c_float)]
+
+
+class GroupNormParams(C.Structure):
+    _fields_ = [("gamma", C.c_void_p), ("beta", C.c_void_p)]
+
+
 ROW_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
+TOKEN_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 4}
 ACTIVATIONS = {"none": 0, "gelu": 1}
+TOKEN_ACTIVATIONS = {"none": 0, "gelu": 1, "silu": 2, "relu": 3}
 NORMS = {"none": 0, "layer": 1, "rms": 2}
 MOST_INT = 2**31 - 1
 
@@ -131,6 +149,15 @@ def load():
         L.mixaq_scaled_linear_forward.argtypes = [C.c_void_p, C.POINTER(Rows), C.c_int32, C.POINTER(Rows), C.c_void_p, C.c_size_t, C.c_void_p]
         L.mixaq_residual_norm.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows),
                                           C.c_int32, C.c_void_p]
+        L.mixaq_token_quantize.argtypes = [C.POINTER(Rows), C.c_int32, C.c_int32, C.POINTER(Rows), C.c_void_p]
+        L.mixaq_token_linear_create.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p)]
+        L.mixaq_token_linear_destroy.argtypes = [C.c_void_p]
+        L.mixaq_token_linear_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.mixaq_token_linear_forward.argtypes = [C.c_void_p, C.POINTER(Rows), C.c_int32, C.POINTER(Rows), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mixaq_token_linear_forward_grouped.argtypes = [C.c_void_p, C.POINTER(Rows), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(Rows),
+                                                         C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mixaq_group_norm_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_size_t)]
+        L.mixaq_group_norm.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(Rows), C.POINTER(Rows), C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
         L.mixaq_block_set_fused.argtypes = [C.c_void_p, C.c_int32]
         L.mixaq_kernel_name.restype = C.c_char_p
         L.mixaq_kernel_name.argtypes = [C.c_int32]
@@ -526,7 +553,195 @@ def mixaq_residual_norm(norm, x, branch=None, y=None, out=None, out_scales=None,
     return y, out
 
 
+# ---------------------------------------------------------------- linear layers on int8 codes with a scale a token, group norm
+def _token_rows(t, name, device, scales=None):
+    """A 2-D tensor on `device` as a mixaq_rows; an int8 one comes with its scales, float [rows]."""
+    if t.dtype is torch.float8_e4m3fn:
+        raise ValueError("%s must be values or int8 codes, not float8_e4m3fn" % name)
+    if t.dtype is not torch.int8:
+        if scales is not None:
+            raise ValueError("%s is not int8, but scales are given" % name)
+        return _rows(t, name, device)
+    if len(t.shape) != 2:
+        raise ValueError("%s must be a 2-D tensor" % name)
+    rows, cols = t.shape
+    if rows > MOST_INT or cols > MOST_INT:
+        raise ValueError("%s is %d x %d: calls take up to 2^30 rows of less than 2^31 columns" % (name, rows, cols))
+    row, col = t.stride()
+    if col != 1 and cols > 1:
+        raise ValueError("%s: the codes of a row must be adjacent (strides %d, %d)" % (name, row, col))
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current device (it is on %s)" % (name, t.device))
+    if scales is None:
+        raise ValueError("%s is int8: its scales are missing" % name)
+    if scales.dtype is not torch.float32 or scales.shape != (rows,) or (rows > 1 and scales.stride(0) != 1):
+        raise ValueError("%s's scales must be float32 of shape (%d,) side by side (got %s, %s)" % (name, rows, scales.dtype, tuple(scales.shape)))
+    if scales.get_device() != device:
+        raise ValueError("%s's scales must be on the current device (they are on %s)" % (name, scales.device))
+    if rows < 2:                                          # the stride of a single row means nothing
+        row = -(-cols // 16) * 16
+    return Rows(t.data_ptr(), row, 4, scales.data_ptr(), 0)
+
+
+def _room_for_16(t, name, stride):
+    """A layer reads a row's codes 16 at a time, those of the last row too."""
+    rows, cols = t.shape
+    if cols % 16 and rows and t.storage_offset() + (rows - 1) * stride + -(-cols // 16) * 16 > t.untyped_storage().nbytes():
+        raise ValueError("%s's last row has no room for its %d codes rounded up to 16 (alloc_token_codes leaves it)" % (name, cols))
+
+
+def _workspace(workspace, device):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device:
+        raise ValueError("workspace must be on the current device (it is on %s)" % workspace.device)
+    if not workspace.is_contiguous():                     # (its bytes would not be those that follow its first)
+        raise ValueError("workspace must be contiguous (strides %s)" % (tuple(workspace.stride()),))
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _list(t, name, dtype, count, device):
+    """The address of a list on `device`."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != (count,) or not t.is_contiguous():
+        raise ValueError("%s must be contiguous %s of shape (%d,) (got %s, %s)" % (name, dtype, count, t.dtype, tuple(t.shape)))
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current device (it is on %s)" % (name, t.device))
+    return t.data_ptr()
+
+
+def mixaq_token_quantize(x, codes, scales, stream=None):
+    """x [rows, cols] values -> codes int8 [rows, cols], scales float [rows]."""
+    if codes.dtype is not torch.int8:
+        raise ValueError("codes must be int8 (got %s)" % codes.dtype)
+    if codes.shape != x.shape:
+        raise ValueError("codes have the shape %s, x %s" % (tuple(codes.shape), tuple(x.shape)))
+    at = _on_device(x, "x")
+    a, q = _rows(x, "x", at), _token_rows(codes, "codes", at, scales)
+    _check(load().mixaq_token_quantize(a, x.shape[0], x.shape[1], q, _stream_of(stream, at)))
+    return codes, scales
+
+
+def mixaq_token_linear_create(w, s_w, bias=None, activation="none", experts=1, stream=None):
+    """w: int8 [experts * N, K], s_w: float [experts * N] as of mixaq_token_quantize; bias: float [experts * N] or None; activation: "none", "gelu",
+    "silu" or "relu".  Returns an opaque handle; w, s_w and bias may be released."""
+    if w.dtype is not torch.int8:
+        raise ValueError("w must be int8 (got %s)" % w.dtype)
+    if not 1 <= experts <= MOST_INT or w.shape[0] % experts:
+        raise ValueError("w has %d rows, which are no %d matrices" % (w.shape[0], experts))
+    at = _on_device(w, "w")
+    p = TokenLinearParams(_token_rows(w, "w", at, s_w), _ptr(_vector(bias, "bias", (w.shape[0],))))
+    d = TokenLinearDesc(w.shape[1], w.shape[0] // experts, experts, _choice(TOKEN_ACTIVATIONS, activation, "activation"))
+    out = C.c_void_p()
+    _check(load().mixaq_token_linear_create(C.byref(d), C.byref(p), _stream_of(stream, at), C.byref(out)))
+    out.K, out.N, out.experts = d.K, d.N, experts
+    return out
+
+
+def mixaq_token_linear_destroy(h):
+    _check(load().mixaq_token_linear_destroy(h))
+
+
+def mixaq_token_linear_workspace_bytes(h, x_rows, x_dtype):
+    if x_rows > MOST_INT:
+        raise ValueError("calls take up to 2^30 rows (got %d)" % x_rows)
+    if x_dtype not in TOKEN_TYPES:
+        raise ValueError("x must be of float32, float16, bfloat16 or int8 (got %s)" % x_dtype)
+    n = C.c_size_t()
+    _check(load().mixaq_token_linear_workspace_bytes(h, x_rows, TOKEN_TYPES[x_dtype], C.byref(n)))
+    return n.value
+
+
+def _token_layer_args(h, x, y, x_scales, workspace):
+    if x.shape[1:] != (h.K,) or y.shape[1:] != (h.N,) or len(y.shape) != 2:
+        raise ValueError("x %s, y %s do not fit a layer of %d inputs and %d outputs" % (tuple(x.shape), tuple(y.shape), h.K, h.N))
+    at = _on_device(x, "x")
+    a, b = _token_rows(x, "x", at, x_scales), _rows(y, "y", at)
+    if a.type == 4:
+        _room_for_16(x, "x", a.stride)
+    return at, a, b, _workspace(workspace, at)
+
+
+def mixaq_token_linear_forward(h, x, y, x_scales=None, workspace=None, stream=None):
+    """x [rows, K] values, or int8 with its scales -> y [rows, N] values."""
+    rows = x.shape[0]
+    if y.shape[0] != rows:
+        raise ValueError("x has %d rows, y %d" % (rows, y.shape[0]))
+    at, a, b, (ws, n) = _token_layer_args(h, x, y, x_scales, workspace)
+    _check(load().mixaq_token_linear_forward(h, a, rows, b, ws, n, _stream_of(stream, at)))
+    return y
+
+
+def mixaq_token_linear_forward_grouped(h, x, offsets, y, x_scales=None, gather=None, row_weights=None, workspace=None, stream=None):
+    """y[r] = row_weights[r] * act(x[gather[r]] w_e^T + bias_e) for the rows offsets[e] .. offsets[e + 1] - 1 of every expert e.  x [x_rows, K]
+    values, or int8 with its scales; y [rows, N] values; offsets: int32 [experts + 1]; gather: int32 [rows] or None; row_weights: float [rows] or
+    None.  Rows of y that no expert has, and those whose index is no row of x, are left as they were."""
+    x_rows, rows = x.shape[0], y.shape[0]
+    at, a, b, (ws, n) = _token_layer_args(h, x, y, x_scales, workspace)
+    lists = (_list(offsets, "offsets", torch.int32, h.experts + 1, at), _list(gather, "gather", torch.int32, rows, at),
+             _list(row_weights, "row_weights", torch.float32, rows, at))
+    _check(load().mixaq_token_linear_forward_grouped(h, a, x_rows, *lists, b, rows, ws, n, _stream_of(stream, at)))
+    return y
+
+
+class GroupNorm:
+    """What mixaq_group_norm takes besides the rows; keeps its vectors alive."""
+
+    def __init__(self, desc, params, vectors):
+        self.desc, self.params, self.vectors = desc, params, vectors
+        self.channels, self.rows_per_image = desc.C, desc.rows_per_image
+        self.args = C.byref(desc), C.byref(params)
+        self.device = next((v.get_device() for v in vectors if v is not None), None)      # None: no vectors
+
+
+def make_group_norm(channels, groups, rows_per_image, eps=1e-5, gamma=None, beta=None, activation="none"):
+    """gamma, beta: float [C] or None; activation: "none", "gelu", "silu" or "relu"."""
+    for v, name in ((channels, "channels"), (groups, "groups"), (rows_per_image, "rows_per_image")):
+        if not 1 <= v <= MOST_INT:
+            raise ValueError("%s must be positive and below 2^31 (got %d)" % (name, v))
+    vectors = [_vector(gamma, "gamma", (channels,)), _vector(beta, "beta", (channels,))]
+    desc = GroupNormDesc(channels, groups, rows_per_image, _choice(TOKEN_ACTIVATIONS, activation, "activation"), eps)
+    return GroupNorm(desc, GroupNormParams(*[_ptr(v) for v in vectors]), vectors)
+
+
+def mixaq_group_norm_workspace_bytes(norm, rows):
+    if rows > MOST_INT:
+        raise ValueError("calls take up to 2^30 rows (got %d)" % rows)
+    n = C.c_size_t()
+    _check(load().mixaq_group_norm_workspace_bytes(norm.args[0], rows, C.byref(n)))
+    return n.value
+
+
+def mixaq_group_norm(norm, x, y, y_scales=None, workspace=None, stream=None):
+    """x [images * rows_per_image, C] values -> y, the same shape: values, or int8 with its scales."""
+    rows = x.shape[0]
+    if x.shape != (rows, norm.channels) or y.shape != x.shape:
+        raise ValueError("x and y must be of shape (rows, %d) (got %s, %s)" % (norm.channels, tuple(x.shape), tuple(y.shape)))
+    at = _on_device(x, "x")
+    if norm.device is not None and norm.device != at:
+        raise ValueError("x is on %s, but the norm's vectors are on device %d" % (x.device, norm.device))
+    ws, n = _workspace(workspace, at)
+    _check(load().mixaq_group_norm(*norm.args, _rows(x, "x", at), _token_rows(y, "y", at, y_scales), rows, ws, n, _stream_of(stream, at)))
+    return y
+
+
 # ---------------------------------------------------------------- memory helpers (no arithmetic)
+def alloc_token_codes(rows, cols, device="cuda:0"):
+    """Room for int8 codes whose rows start at multiples of 16 bytes, and for their scales."""
+    return torch.zeros((rows, -(-cols // 16) * 16), dtype=torch.int8, device=device)[:, :cols], torch.empty(rows, dtype=torch.float32, device=device)
+
+
+def alloc_token_linear_workspace(h, x_rows, x_dtype, device="cuda:0"):
+    """None where the call needs none."""
+    n = mixaq_token_linear_workspace_bytes(h, x_rows, x_dtype)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def alloc_group_norm_workspace(norm, rows, device="cuda:0"):
+    return torch.empty(mixaq_group_norm_workspace_bytes(norm, rows), dtype=torch.uint8, device=device)
+
+
 def alloc_codes(rows, cols, block_rows=1, device="cuda:0"):
     """Room for codes whose rows start at multiples of 16 bytes, and for their scales."""
     codes = torch.zeros((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)[:, :cols]

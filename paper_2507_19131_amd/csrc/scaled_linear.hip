@@ -1,5 +1,6 @@
 // Linear layers on 8-bit float codes with a scale per 128 columns: y = act(x w^T + bias), the products on the e4m3 matrix
 // instruction of gfx950, 128 deep, which is one block of scales.
+#include "activations.h"
 #include "scaled.h"
 #include "scaled_forms.h"
 
@@ -64,23 +65,6 @@ __global__ __launch_bounds__(256) void pack_vectors_kernel(const float* s, long 
 }
 
 // ---- the end of a tile ------------------------------------------------------------------------------------------------
-// GELU(v) = v Phi(v), Phi(v) = 1 / (1 + 2^-t), t = v P(v^2): the logarithm of Phi's odds is odd and smooth, P its fit by weighted least
-// squares on 0 < v < 7 (at most 9.4e-8 |v| off; beyond, t only grows).  13 instructions, by Abramowitz and Stegun's erfc, which is as exact,
-// 18.  The median keeps the last product at -infinity from being 0 times infinity; a NaN comes through the other factor.
-__device__ __forceinline__ float gelu(float v)
-{
-    const float u = v * v;
-    float p = fmaf(u, 0x1.67ab6cp-28f, -0x1.9e7b64p-22f);
-    p = fmaf(p, u, 0x1.80c28cp-17f);
-    p = fmaf(p, u, -0x1.4e76fep-13f);
-    p = fmaf(p, u, -0x1.8fb242p-14f);
-    p = fmaf(p, u, 0x1.ad6ad0p-4f);
-    p = fmaf(p, u, 0x1.26aebcp+1f);
-    float top = INFINITY;
-    asm("" : "+v"(top));                                  // (a constant, and the compiler makes two maxima of the median)
-    return __builtin_amdgcn_fmed3f(v, -0x1.fffffep+127f, top) * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * p));
-}
-
 // The end of a wave's ROWS rows and 128 outputs: a lane holds those of one row, the bias in them, in RUNS runs of 16 neighbouring ones, run i from
 // column offset(i) of block nb on; the lanes l, l + ROWS, .. hold the whole row.  Through LDS (`turn`: 16 or 32 rows x 256 bytes of the
 // wave's own), so that a store covers whole lines: from the lanes themselves it would touch 32 rows with 32 bytes each (268324 x 128 x 512 of bf16
