@@ -1,6 +1,7 @@
 // Linear layers on int8 codes with a scale per token and channel: y = act(x w^T + bias), the products on the int8 matrix instructions of gfx950,
 // the sums exact; for one matrix, or for rows sorted by expert and a matrix for each.
 #include "token.h"
+#include "token_forms.h"
 
 #include <algorithm>
 #include <new>
@@ -227,6 +228,261 @@ __global__ __launch_bounds__(NW * 64) void token_few_kernel(TokenArgs A, int per
     }
 }
 
+// ---- both operands through LDS ------------------------------------------------------------------------------------------
+// A workgroup of WM x WN waves computes 32 MT WM rows times 128 WN outputs, a wave 32 MT rows times one block of 128 outputs.  K goes in stages of one
+// block of 128 through two LDS buffers filled by direct loads; a stage travels under the products of the one before it.
+// Rows of x lie in LDS as 8 chunks of 16 bytes whose places are turned by half the row's number, so that the 16 lanes that are served
+// together (16 rows, one chunk) meet all 64 banks.
+// The direct loads are asm: as a builtin every LDS read behind them waits for all of them.  They do nothing for stages from `end` on, which the asm finds out: a
+// branch around it would be one in the middle of a stage.
+#define MIXAQ_REQUEST(ADDRESS_, ...)                                                                                                      \
+    int m0; /* given back: the compiler does not let an asm statement change it */                                                       \
+    asm volatile("s_cmp_ge_i32 %2, %3\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 " ADDRESS_ \
+                 "\n\ts_mov_b32 m0, %0\n.Lskip%=:" : "=&s"(m0) : "s"(lds_dst), "s"(stage), "s"(end), __VA_ARGS__ : "memory", "scc")
+__device__ __forceinline__ void request_at(const uint8_t* lane_src, unsigned lds_dst, int stage, int end) { MIXAQ_REQUEST("%4, off", "v"(lane_src)); }
+__device__ __forceinline__ void request_run(const uint8_t* uniform_src, unsigned lane_bytes, unsigned lds_dst, int stage, int end)
+{
+    MIXAQ_REQUEST("%4, %5", "v"(lane_bytes), "s"(uniform_src));
+}
+#undef MIXAQ_REQUEST
+__device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)p; }
+
+// Of instructions of 32 x 32 x 32 the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, lane half h takes the 16-byte chunk 2 c + h of a row's 128 bytes in
+// step c.  Result e is row 8 (e / 4) + 4 h + e % 4: of the outputs, by output_of, number 4 (2 (T % 2) + e / 8) + e % 4 of
+// run 2 (e / 4 % 2) + h of 16, in half T / 2 of the block.
+__device__ __forceinline__ int run_of(int i, int h) { return (i >> 1) * 64 + (2 * (i & 1) + h) * 16; }
+__device__ __forceinline__ constexpr int place_of(int T, int e) { return ((T >> 1) * 2 + (e >> 2 & 1)) * 16 + ((T & 1) * 2 + (e >> 3)) * 4 + (e & 3); }
+
+// The end of a wave's 32 rows and 128 outputs: a lane holds those of one row, in 4 runs of 16 neighbouring ones, the lanes l and l + 32 the whole row.  Through LDS
+// (`turn`: 32 rows x 256 bytes of the wave's own), so that a store covers whole lines; its 16-byte pieces are turned by the row, so that
+// neither side meets a bank twice.  kept: a bit for each row that is stored.
+template <int YT>
+__device__ __forceinline__ void store_rows(const TokenArgs& A, const float (&v)[64], int nb, int row0, unsigned kept, v4i* turn)
+{
+    using T = typename TypeOf<YT>::T;
+    constexpr int ES = sizeof(T), PASSES = ES / 2;
+    const int lane = threadIdx.x & 63, own = lane & 31, h = lane >> 5;
+    auto in_order = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };           // among the lanes of the wave, which runs in step
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+#pragma unroll
+        for (int i = pass * 4 / PASSES; i < (pass + 1) * 4 / PASSES; ++i) {
+            T t[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) t[e] = (T)v[i * 16 + e];
+            const int p = run_of(i, h) * ES % 256 / 16;
+#pragma unroll
+            for (int q = 0; q < ES; ++q) __builtin_memcpy(&turn[own * 16 + ((p + q) ^ (own & 15))], (const uint8_t*)t + q * 16, 16);
+        }
+        in_order();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int r = k * 4 + (lane >> 4), p = lane & 15, n = nb * SBLOCK + (pass * 256 + p * 16) / ES;
+            const v4i piece = turn[r * 16 + (p ^ (r & 15))];
+            if (!(kept >> r & 1)) continue;
+            T* const to = (T*)A.y + (long long)(row0 + r) * A.ldy + n;
+            if (n + 16 / ES <= A.N) __builtin_memcpy(to, &piece, 16);
+            else {
+                T t[16 / ES];
+                __builtin_memcpy(t, &piece, 16);
+#pragma unroll
+                for (int e = 0; e < 16 / ES; ++e)
+                    if (n + e < A.N) to[e] = t[e];
+            }
+        }
+        in_order();
+    }
+}
+
+// Inclusive sums over the lanes of a wave.
+__device__ __forceinline__ int scan64(int v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(v, d, 64);
+        v += lane >= d ? o : 0;
+    }
+    return v;
+}
+// Row tiles of TM rows, expert after expert: how many there are in all, and of the t-th its expert and its rows.  By every wave for itself.
+template <int TM>
+struct SortedTiles {
+    int total = 0, kept = 0;                                                 // kept: of the last 64 experts looked at
+    __device__ int tiles(const TokenArgs& A, int e)
+    {
+        if (e >= A.experts) return 0;
+        int first, end;
+        rows_of(A, e, first, end);
+        return (end - first + TM - 1) / TM;
+    }
+    __device__ void count(const TokenArgs& A, int most)                      // at most `most`, whatever the offsets
+    {
+        for (int e0 = 0; e0 < A.experts; e0 += 64) {
+            kept = scan64(tiles(A, e0 + (threadIdx.x & 63)));
+            total = min(total + __builtin_amdgcn_readlane(kept, 63), most);
+        }
+    }
+    __device__ void find(const TokenArgs& A, int t, int& e, int& first, int& end)
+    {
+        int before = 0;
+        first = end = 0;
+        for (int e0 = 0; e0 < A.experts; e0 += 64) {                         // (t < total: some expert has it)
+            if (A.experts > 64) kept = scan64(tiles(A, e0 + (threadIdx.x & 63)));
+            const unsigned long long behind = __ballot(before + kept > t);
+            if (behind) {
+                const int l = __ffsll((long long)behind) - 1;
+                e = __builtin_amdgcn_readfirstlane(e0 + l);
+                const int skipped = before + (l ? __builtin_amdgcn_readlane(kept, l - 1) : 0);
+                rows_of(A, e, first, end);
+                first += (t - skipped) * TM;
+                end = min(end, first + TM);
+                return;
+            }
+            before += __builtin_amdgcn_readlane(kept, 63);
+        }
+    }
+};
+
+constexpr int GROUP_M = 4;                        // row tiles that run beside one another
+
+template <int YT, int MT, int WM, int WN, bool SORTED>
+__global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
+{
+    constexpr int W = WM * WN, TM = 32 * MT * WM;
+    constexpr int XP = TM / 8, WP = WN * 16, XL = XP / W, WL = WP / W;       // 1 KB pieces of a stage, of x and of w, and a wave's
+    static_assert(XP % W == 0 && WP % W == 0 && XL % 2 == 0, "whole pieces a wave, the parity of a piece that of i");
+    __shared__ v4i xs[2][XP * 64], ws[2][WP * 64];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
+    const int wm = wave / WN, wn = wave % WN, KB = A.KB;
+    // a run of tiles per XCD, so that what its CUs read at one time meets in its L2: in groups of GROUP_M row tiles with all their outputs, or row
+    // tile by row tile
+    SortedTiles<TM> sorted;
+    if (SORTED) sorted.count(A, tiles_m);
+    const int tiles = (SORTED ? sorted.total : tiles_m) * tiles_n, per_xcd = (tiles + 7) / 8;
+    const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per_xcd || t >= tiles) return;             // the whole workgroup
+    int tn, first, end, expert = 0;
+    if (SORTED) {
+        const int rt = by(t);
+        tn = t - rt * tiles_n;
+        sorted.find(A, rt, expert, first, end);
+    } else {
+        const int group = by(t), in = t - group * GROUP_M * tiles_n, gm = min(GROUP_M, tiles_m - group * GROUP_M);
+        tn = in / gm;
+        first = (group * GROUP_M + in - tn * gm) * TM;
+        end = min(A.M, first + TM);
+    }
+    const int nb0 = tn * WN, nb = nb0 + wn;
+
+    // what this wave requests: rows (wave XL + i) 8 + lane / 8 of x, whose lanes take the chunk that belongs in their place, and pieces
+    // wave WL + i of w
+    const int chunk[2] = {((lane & 7) ^ (lane >> 4)) * 16, ((lane & 7) ^ (lane >> 4) ^ 4) * 16};     // of even and of odd pieces
+    const uint8_t* from[XL];
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+        const int r = min(first + (wave * XL + i) * 8 + (lane >> 3), end - 1);
+        from[i] = (const uint8_t*)A.x + (long long)(SORTED ? max(source_of(A, r), 0) : r) * A.ldx;
+    }
+    const uint8_t* const wb = A.w + ((long long)expert * A.NB + min(nb0 + wave * WL / 16, A.NB - 1)) * KB * (8 * TILE_BYTES) + wave * WL % 16 * 1024;
+    const unsigned lx = lds_address(xs), lw = lds_address(ws);
+    auto request = [&](int kb, int i) {                                      // chunks behind a row's end: the row's first, the weights there are zero
+        if (i < XL) {
+            const int k = kb * SBLOCK + chunk[i & 1];
+            request_at(from[i] + (k < A.K ? k : 0), lx + ((kb & 1) * XP + wave * XL + i) * 1024, kb, KB);
+        } else {
+            i -= XL;
+            request_run(wb + (long long)kb * (8 * TILE_BYTES) + i * 1024, lane * 16, lw + ((kb & 1) * WP + wave * WL + i) * 1024, kb, KB);
+        }
+    };
+    auto landed = [&] {                                                      // every wave's requests, and its reads of the other buffer have returned
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < XL + WL; ++i) request(0, i);
+    const int m0 = wm * 32 * MT;
+    float sx[MT];
+    unsigned kept[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {                                           // (needed at the end, on their way meanwhile)
+        const int r = first + m0 + m * 32 + j, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
+        sx[m] = A.sx[max(src, 0)];
+        kept[m] = (unsigned)__ballot(r < end && src >= 0);
+    }
+    v16i acc[MT][4] = {};
+    v4i x[2][MT], w[2][4];
+    auto read = [&](int kb, int c, int i) {                                  // operand i of step c
+        if (i < MT) {
+            const int r = m0 + i * 32 + j;
+            x[c & 1][i] = xs[kb & 1][r * 8 + ((2 * c + h) ^ (r >> 1 & 7))];
+        } else {
+            const int T = i - MT;
+            w[c & 1][T] = ws[kb & 1][wn * 1024 + ((2 * T + (j >> 4)) * 2 + (c >> 1)) * 64 + ((2 * c + h) & 3) * 16 + (j & 15)];
+        }
+    };
+    landed();
+#pragma unroll
+    for (int i = 0; i < XL + WL; ++i) request(1, i);
+#pragma unroll
+    for (int i = 0; i < MT + 4; ++i) read(0, 0, i);
+    // Of each stage four steps of 32.  What a step's products need is read under those of the step before; behind the last read of a stage the waves
+    // meet, and its buffer is requested anew.  The last stage reads on like the others, for nobody.
+#pragma unroll 1
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (c == 3) landed();
+            constexpr int P = 4 * MT;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int T = p / MT, m = p % MT;
+                __builtin_amdgcn_sched_barrier(0);
+                acc[m][T] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c & 1][T], x[c & 1][m], acc[m][T], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = p * (MT + 4) / P; i < (p + 1) * (MT + 4) / P; ++i) read(c == 3 ? kb + 1 : kb, (c + 1) & 3, i);
+                if (c == 3) {
+#pragma unroll
+                    for (int i = p * (XL + WL) / P; i < (p + 1) * (XL + WL) / P; ++i) request(kb + 2, i);
+                }
+            }
+        }
+    }
+    landed();                                                                // (and the last reads for nobody)
+    if (nb >= A.NB) return;
+    static_assert(2 * XP * 64 >= W * 512, "room for a wave's 32 rows of 256 bytes");
+    v4i* const turn = &xs[0][0] + wave * 512;
+    const float* const sw = A.sw + ((long long)expert * A.NB + nb) * SBLOCK;
+    const float* const bias = A.bias + ((long long)expert * A.NB + nb) * SBLOCK;
+    float s[64], b[64];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __builtin_memcpy(&s[i * 16], sw + run_of(i, h), 64);
+        __builtin_memcpy(&b[i * 16], bias + run_of(i, h), 64);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        float v[64];
+#pragma unroll
+        for (int T = 0; T < 4; ++T)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int at = place_of(T, e);
+                v[at] = fmaf((float)acc[m][T][e], sx[m] * s[at], b[at]);
+            }
+        activate(v, A.act);
+        const int row0 = first + m0 + m * 32;
+        if (SORTED && A.weights) {
+            const float weight = A.weights[min(row0 + j, end - 1)];
+#pragma unroll
+            for (int e = 0; e < 64; ++e) v[e] *= weight;
+        }
+        store_rows<YT>(A, v, nb, row0, kept[m], turn);
+    }
+}
+
 // Quantizes x first where it is given as values; behind the checks of the product that follows.
 int quantize_first(const TokenArgs& A, const mixaq_rows* values, hipStream_t st)
 {
@@ -248,22 +504,42 @@ int launch_few(const TokenArgs& A, const mixaq_rows* values, hipStream_t st)
     return MIXAQ_OK;
 }
 
-template <int YT, bool SORTED>
-int launch_linear(const TokenArgs& A, int x_type, const mixaq_rows* values, hipStream_t st)
+template <int YT, int MT, int WM, int WN, bool SORTED>
+int launch_tiles(const TokenArgs& A, const mixaq_rows* values, hipStream_t st)
 {
+    constexpr int TM = 32 * MT * WM;
+    const int tiles_n = (A.NB + WN - 1) / WN;
+    const long long tiles_m = ((long long)A.M + TM - 1) / TM + (SORTED ? std::min(A.experts, A.M) : 0);      // (every expert's last tile may be cut)
+    const long long blocks = (tiles_m * tiles_n + 7) / 8 * 8;
+    if (blocks * WM * WN * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
+    const int rc = quantize_first(A, values, st);
+    if (rc) return rc;
+    hipLaunchKernelGGL((token_tile_kernel<YT, MT, WM, WN, SORTED>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, (int)tiles_m, tiles_n,
+                       FastDiv(SORTED ? tiles_n : GROUP_M * tiles_n));
+    HIP_TRY(hipGetLastError());
+    return MIXAQ_OK;
+}
+
+template <int YT, bool SORTED>
+int launch_linear(const TokenArgs& A, TokenForm form, int x_type, const mixaq_rows* values, hipStream_t st)
+{
+    switch (form) {
+    case TOKEN_TILE: return launch_tiles<YT, 1, 4, 1, SORTED>(A, values, st);
+    case TOKEN_LARGE: return launch_tiles<YT, 4, 2, 2, SORTED>(A, values, st);
+    case TOKEN_MID: return launch_few<MIXAQ_I8, YT, 2, 2, 8, SORTED>(A, values, st);
+    case TOKEN_SPLIT: return launch_few<MIXAQ_I8, YT, 4, 4, 4, SORTED>(A, values, st);
+    case TOKEN_FEW: break;
+    }
     if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT, 1, 1, 8, SORTED>(A, values, st);
     if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT, 1, 1, 8, SORTED>(A, values, st);
     if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT, 1, 1, 8, SORTED>(A, values, st);
     return launch_few<MIXAQ_I8, YT, 1, 1, 8, SORTED>(A, values, st);
 }
 
-// Whether values are quantized on their way into the product
-bool quantized_inside(int x_rows) { return x_rows <= 16; }
-
 // the workspace: codes and scales of x, where it is given as values and not quantized on its way into the product
 size_t workspace_of(const mixaq_token_linear* h, int32_t x_rows, int32_t x_type)
 {
-    if (x_type == MIXAQ_I8 || x_rows == 0 || quantized_inside(x_rows)) return 0;
+    if (x_type == MIXAQ_I8 || x_rows == 0 || token_quantized_inside(x_rows, h->KB)) return 0;
     return align256((size_t)x_rows * round_up16(h->d.K)) + align256((size_t)x_rows * 4);
 }
 
@@ -353,15 +629,16 @@ int forward(const mixaq_token_linear* h, const mixaq_rows* x, int32_t x_rows, co
     A.M = rows; A.x_rows = x_rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
     A.act = h->d.activation; A.experts = h->d.experts;
     const mixaq_rows* const values = need ? x : nullptr;
+    const TokenForm form = token_form(rows, A.KB, A.NB, h->d.experts, sorted != nullptr, codes.type != MIXAQ_I8);
     if (sorted) {
         A.offsets = sorted->offsets; A.gather = sorted->gather; A.weights = sorted->weights;
-        if (y->type == MIXAQ_F32) return launch_linear<MIXAQ_F32, true>(A, codes.type, values, st);
-        if (y->type == MIXAQ_F16) return launch_linear<MIXAQ_F16, true>(A, codes.type, values, st);
-        return launch_linear<MIXAQ_BF16, true>(A, codes.type, values, st);
+        if (y->type == MIXAQ_F32) return launch_linear<MIXAQ_F32, true>(A, form, codes.type, values, st);
+        if (y->type == MIXAQ_F16) return launch_linear<MIXAQ_F16, true>(A, form, codes.type, values, st);
+        return launch_linear<MIXAQ_BF16, true>(A, form, codes.type, values, st);
     }
-    if (y->type == MIXAQ_F32) return launch_linear<MIXAQ_F32, false>(A, codes.type, values, st);
-    if (y->type == MIXAQ_F16) return launch_linear<MIXAQ_F16, false>(A, codes.type, values, st);
-    return launch_linear<MIXAQ_BF16, false>(A, codes.type, values, st);
+    if (y->type == MIXAQ_F32) return launch_linear<MIXAQ_F32, false>(A, form, codes.type, values, st);
+    if (y->type == MIXAQ_F16) return launch_linear<MIXAQ_F16, false>(A, form, codes.type, values, st);
+    return launch_linear<MIXAQ_BF16, false>(A, form, codes.type, values, st);
 }
 
 }  // namespace
