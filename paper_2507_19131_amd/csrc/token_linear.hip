@@ -229,22 +229,20 @@ __global__ __launch_bounds__(NW * 64) void token_few_kernel(TokenArgs A, int per
 }
 
 // ---- both operands through LDS ------------------------------------------------------------------------------------------
-// A workgroup of WM x WN waves computes 32 MT WM rows times 128 WN outputs, a wave 32 MT rows times one block of 128 outputs.  K goes in stages of one
-// block of 128 through two LDS buffers filled by direct loads; a stage travels under the products of the one before it.
-// Rows of x lie in LDS as 8 chunks of 16 bytes whose places are turned by half the row's number, so that the 16 lanes that are served
+// A workgroup of WM x WN waves computes 32 MT WM rows times 128 WN outputs, a wave 32 MT rows times one block of 128 outputs.  K goes in stages of 64 through a
+// ring of four LDS buffers filled by direct loads, three stages ahead of the products.
+// Rows of x lie in LDS as 4 chunks of 16 bytes whose places are turned by a fourth of the row's number, so that the 16 lanes that are served
 // together (16 rows, one chunk) meet all 64 banks.
 // The direct loads are asm: as a builtin every LDS read behind them waits for all of them.  They do nothing for stages from `end` on, which the asm finds out: a
 // branch around it would be one in the middle of a stage.
-#define MIXAQ_REQUEST(ADDRESS_, ...)                                                                                                      \
-    int m0; /* given back: the compiler does not let an asm statement change it */                                                       \
-    asm volatile("s_cmp_ge_i32 %2, %3\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 " ADDRESS_ \
-                 "\n\ts_mov_b32 m0, %0\n.Lskip%=:" : "=&s"(m0) : "s"(lds_dst), "s"(stage), "s"(end), __VA_ARGS__ : "memory", "scc")
-__device__ __forceinline__ void request_at(const uint8_t* lane_src, unsigned lds_dst, int stage, int end) { MIXAQ_REQUEST("%4, off", "v"(lane_src)); }
-__device__ __forceinline__ void request_run(const uint8_t* uniform_src, unsigned lane_bytes, unsigned lds_dst, int stage, int end)
+// Two pieces one behind the other in LDS.
+__device__ __forceinline__ void request2(const uint8_t* uniform_src, unsigned first, unsigned second, unsigned lds_dst, int stage, int end)
 {
-    MIXAQ_REQUEST("%4, %5", "v"(lane_bytes), "s"(uniform_src));
+    int m0;                                                                  // given back: the compiler does not let an asm statement change it
+    asm volatile("s_cmp_ge_i32 %5, %6\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
+                 "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0\n.Lskip%=:"
+                 : "=&s"(m0) : "v"(first), "v"(second), "s"(uniform_src), "s"(lds_dst), "s"(stage), "s"(end) : "memory", "scc");
 }
-#undef MIXAQ_REQUEST
 __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(size_t)(const __attribute__((address_space(3))) char*)p; }
 
 // Of instructions of 32 x 32 x 32 the packed tiles 2 T and 2 T + 1 are rows 0 .. 31 of the T-th, lane half h takes the 16-byte chunk 2 c + h of a row's 128 bytes in
@@ -346,15 +344,32 @@ struct SortedTiles {
 
 constexpr int GROUP_M = 4;                        // row tiles that run beside one another
 
+// Waits until of the stages that this wave has requested, R loads each, at most min(CAP, left) are on their way.
+template <int R, int CAP>
+__device__ __forceinline__ void wait_stages(int left)
+{
+    static_assert(CAP == 2 || CAP == 3, "");
+    if constexpr (CAP == 3)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_cmp_lt_i32 %0, 1\n\ts_cbranch_scc1 .Lnone%=\n\ts_cmp_lt_i32 %0, 2\n\ts_cbranch_scc1 .Lone%=\n\ts_cmp_lt_i32 %0, 3\n\t"
+                     "s_cbranch_scc1 .Ltwo%=\n\ts_waitcnt vmcnt(%3)\n\ts_branch .Ldone%=\n.Ltwo%=:\n\ts_waitcnt vmcnt(%2)\n\ts_branch .Ldone%=\n.Lone%=:\n\t"
+                     "s_waitcnt vmcnt(%1)\n\ts_branch .Ldone%=\n.Lnone%=:\n\ts_waitcnt vmcnt(0)\n.Ldone%=:" :: "s"(left), "n"(R), "n"(2 * R), "n"(3 * R) : "memory", "scc");
+    else
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_cmp_lt_i32 %0, 1\n\ts_cbranch_scc1 .Lnone%=\n\ts_cmp_lt_i32 %0, 2\n\ts_cbranch_scc1 .Lone%=\n\ts_waitcnt vmcnt(%2)\n\t"
+                     "s_branch .Ldone%=\n.Lone%=:\n\ts_waitcnt vmcnt(%1)\n\ts_branch .Ldone%=\n.Lnone%=:\n\ts_waitcnt vmcnt(0)\n.Ldone%=:"
+                     :: "s"(left), "n"(R), "n"(2 * R) : "memory", "scc");
+}
+
+constexpr int DEPTH = 64, RING = 4;               // bytes of K in a stage, stages in LDS
+
 template <int YT, int MT, int WM, int WN, bool SORTED>
 __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
 {
     constexpr int W = WM * WN, TM = 32 * MT * WM;
-    constexpr int XP = TM / 8, WP = WN * 16, XL = XP / W, WL = WP / W;       // 1 KB pieces of a stage, of x and of w, and a wave's
-    static_assert(XP % W == 0 && WP % W == 0 && XL % 2 == 0, "whole pieces a wave, the parity of a piece that of i");
-    __shared__ v4i xs[2][XP * 64], ws[2][WP * 64];
+    constexpr int XP = TM / 16, WP = WN * 8, XL = XP / W, WL = WP / W, R = XL + WL;      // 1 KB pieces of a stage, of x and of w, and a wave's
+    static_assert(XL % 2 == 0 && WL % 2 == 0 && XP % W == 0 && WP % W == 0, "pairs of whole pieces a wave");
+    __shared__ v4i xs[RING][XP * 64], ws[RING][WP * 64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
-    const int wm = wave / WN, wn = wave % WN, KB = A.KB;
+    const int wm = wave / WN, wn = wave % WN, KB = A.KB, stages = (A.K + DEPTH - 1) / DEPTH;
     // a run of tiles per XCD, so that what its CUs read at one time meets in its L2: in groups of GROUP_M row tiles with all their outputs, or row
     // tile by row tile
     SortedTiles<TM> sorted;
@@ -375,84 +390,81 @@ __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kern
     }
     const int nb0 = tn * WN, nb = nb0 + wn;
 
-    // what this wave requests: rows (wave XL + i) 8 + lane / 8 of x, whose lanes take the chunk that belongs in their place, and pieces
-    // wave WL + i of w
-    const int chunk[2] = {((lane & 7) ^ (lane >> 4)) * 16, ((lane & 7) ^ (lane >> 4) ^ 4) * 16};     // of even and of odd pieces
-    const uint8_t* from[XL];
+    // what this wave requests: rows (wave XL + i) 16 + lane / 4 of x, whose lanes take the chunk that belongs in their place, and pieces wave WL + i of w
+    const int chunk = ((lane & 3) ^ (lane >> 4)) * 16, last_chunk = (A.K - 1) & ~15;      // (what stands behind a row's end is the last chunk again, the weights there are zero)
+    const uint8_t* const xb = (const uint8_t*)A.x + (SORTED ? 0 : (long long)first * A.ldx);
+    unsigned from[XL], piece[WL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-        const int r = min(first + (wave * XL + i) * 8 + (lane >> 3), end - 1);
-        from[i] = (const uint8_t*)A.x + (long long)(SORTED ? max(source_of(A, r), 0) : r) * A.ldx;
+        const int r = min(first + (wave * XL + i) * 16 + (lane >> 2), end - 1);
+        from[i] = (unsigned)(SORTED ? max(source_of(A, r), 0) : r - first) * (unsigned)A.ldx;
     }
-    const uint8_t* const wb = A.w + ((long long)expert * A.NB + min(nb0 + wave * WL / 16, A.NB - 1)) * KB * (8 * TILE_BYTES) + wave * WL % 16 * 1024;
+#pragma unroll
+    for (int i = 0; i < WL; ++i) piece[i] = i * TILE_BYTES + lane * 16;
+    const uint8_t* const wb = A.w + ((long long)expert * A.NB + min(nb0 + wave * WL / 8, A.NB - 1)) * KB * (8 * TILE_BYTES) + wave * WL % 8 * TILE_BYTES;
     const unsigned lx = lds_address(xs), lw = lds_address(ws);
-    auto request = [&](int kb, int i) {                                      // chunks behind a row's end: the row's first, the weights there are zero
+    auto request = [&](int ks, int i) {                                      // two pieces
         if (i < XL) {
-            const int k = kb * SBLOCK + chunk[i & 1];
-            request_at(from[i] + (k < A.K ? k : 0), lx + ((kb & 1) * XP + wave * XL + i) * 1024, kb, KB);
+            const unsigned k = min(ks * DEPTH + chunk, last_chunk);
+            request2(xb, from[i] + k, from[i + 1] + k, lx + (ks % RING * XP + wave * XL + i) * 1024, ks, stages);
         } else {
             i -= XL;
-            request_run(wb + (long long)kb * (8 * TILE_BYTES) + i * 1024, lane * 16, lw + ((kb & 1) * WP + wave * WL + i) * 1024, kb, KB);
+            request2(wb + (long long)(ks >> 1) * (8 * TILE_BYTES) + (ks & 1) * 1024, piece[i], piece[i + 1], lw + (ks % RING * WP + wave * WL + i) * 1024, ks, stages);
         }
     };
-    auto landed = [&] {                                                      // every wave's requests, and its reads of the other buffer have returned
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    auto meet = [] {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
 #pragma unroll
-    for (int i = 0; i < XL + WL; ++i) request(0, i);
-    const int m0 = wm * 32 * MT;
-    float sx[MT];
-    unsigned kept[MT];
+    for (int ks = 0; ks < RING; ++ks)
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {                                           // (needed at the end, on their way meanwhile)
-        const int r = first + m0 + m * 32 + j, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
-        sx[m] = A.sx[max(src, 0)];
-        kept[m] = (unsigned)__ballot(r < end && src >= 0);
-    }
+        for (int i = 0; i < R; i += 2) request(ks, i);
+    const int m0 = wm * 32 * MT;
     v16i acc[MT][4] = {};
     v4i x[2][MT], w[2][4];
-    auto read = [&](int kb, int c, int i) {                                  // operand i of step c
-        if (i < MT) {
-            const int r = m0 + i * 32 + j;
-            x[c & 1][i] = xs[kb & 1][r * 8 + ((2 * c + h) ^ (r >> 1 & 7))];
-        } else {
-            const int T = i - MT;
-            w[c & 1][T] = ws[kb & 1][wn * 1024 + ((2 * T + (j >> 4)) * 2 + (c >> 1)) * 64 + ((2 * c + h) & 3) * 16 + (j & 15)];
-        }
+    const v4i* const xr[2] = {&xs[0][(m0 + j) * 4 + (h ^ (j >> 2 & 3))], &xs[0][(m0 + j) * 4 + (h ^ 2 ^ (j >> 2 & 3))]};
+    const v4i* const wr = &ws[0][wn * 512 + (j >> 4) * 64 + h * 16 + (j & 15)];
+    auto read = [&](int ks, int c, int i) {                                  // operand i of step c
+        if (i < MT) x[c][i] = xr[c][ks % RING * (XP * 64) + i * 128];
+        else w[c][i - MT] = wr[ks % RING * (WP * 64) + (i - MT) * 128 + c * 32];
     };
-    landed();
-#pragma unroll
-    for (int i = 0; i < XL + WL; ++i) request(1, i);
+    wait_stages<R, 3>(stages - 1);
+    meet();
 #pragma unroll
     for (int i = 0; i < MT + 4; ++i) read(0, 0, i);
-    // Of each stage four steps of 32.  What a step's products need is read under those of the step before; behind the last read of a stage the waves
+    // Of each stage two steps of 32.  What a step's products need is read under those of the step before; behind the last read of a stage the waves
     // meet, and its buffer is requested anew.  The last stage reads on like the others, for nobody.
 #pragma unroll 1
-    for (int kb = 0; kb < KB; ++kb) {
+    for (int ks = 0; ks < stages; ++ks) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            if (c == 3) landed();
-            constexpr int P = 4 * MT;
+        for (int c = 0; c < 2; ++c) {
+            if (c == 1) {
+                wait_stages<R, 2>(stages - 2 - ks);
+                meet();
+            }
+            constexpr int P = 4 * MT, READS = MT == 1 ? 2 : 1;               // after each of the first products
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const int T = p / MT, m = p % MT;
                 __builtin_amdgcn_sched_barrier(0);
-                acc[m][T] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c & 1][T], x[c & 1][m], acc[m][T], 0, 0, 0);
+                acc[m][T] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c][T], x[c][m], acc[m][T], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = p * (MT + 4) / P; i < (p + 1) * (MT + 4) / P; ++i) read(c == 3 ? kb + 1 : kb, (c + 1) & 3, i);
-                if (c == 3) {
+                for (int i = p * READS; i < (p + 1) * READS; ++i)
+                    if (i < MT + 4) read(c == 1 ? ks + 1 : ks, c ^ 1, i);
+                if (c == 1) {
 #pragma unroll
-                    for (int i = p * (XL + WL) / P; i < (p + 1) * (XL + WL) / P; ++i) request(kb + 2, i);
+                    for (int i = p * R / P; i < (p + 1) * R / P; ++i)
+                        if (i % 2 == 0) request(ks + RING, i);
                 }
             }
         }
     }
-    landed();                                                                // (and the last reads for nobody)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");              // (and the last reads for nobody)
+    meet();
     if (nb >= A.NB) return;
-    static_assert(2 * XP * 64 >= W * 512, "room for a wave's 32 rows of 256 bytes");
+    static_assert(RING * XP * 64 >= W * 512, "room for a wave's 32 rows of 256 bytes");
     v4i* const turn = &xs[0][0] + wave * 512;
     const float* const sw = A.sw + ((long long)expert * A.NB + nb) * SBLOCK;
     const float* const bias = A.bias + ((long long)expert * A.NB + nb) * SBLOCK;
@@ -464,22 +476,23 @@ __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kern
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
+        const int row0 = first + m0 + m * 32, r = row0 + j, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
+        const float sx = A.sx[max(src, 0)];
         float v[64];
 #pragma unroll
         for (int T = 0; T < 4; ++T)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int at = place_of(T, e);
-                v[at] = fmaf((float)acc[m][T][e], sx[m] * s[at], b[at]);
+                const int to = place_of(T, e);
+                v[to] = fmaf((float)acc[m][T][e], sx * s[to], b[to]);
             }
         activate(v, A.act);
-        const int row0 = first + m0 + m * 32;
         if (SORTED && A.weights) {
-            const float weight = A.weights[min(row0 + j, end - 1)];
+            const float weight = A.weights[at];
 #pragma unroll
             for (int e = 0; e < 64; ++e) v[e] *= weight;
         }
-        store_rows<YT>(A, v, nb, row0, kept[m], turn);
+        store_rows<YT>(A, v, nb, row0, (unsigned)__ballot(r < end && src >= 0), turn);
     }
 }
 
@@ -629,7 +642,7 @@ int forward(const mixaq_token_linear* h, const mixaq_rows* x, int32_t x_rows, co
     A.M = rows; A.x_rows = x_rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
     A.act = h->d.activation; A.experts = h->d.experts;
     const mixaq_rows* const values = need ? x : nullptr;
-    const TokenForm form = token_form(rows, A.KB, A.NB, h->d.experts, sorted != nullptr, codes.type != MIXAQ_I8);
+    const TokenForm form = token_form(rows, A.KB, A.NB, h->d.experts, sorted != nullptr, (sorted ? x_rows : 256LL) * A.ldx, codes.type != MIXAQ_I8);
     if (sorted) {
         A.offsets = sorted->offsets; A.gather = sorted->gather; A.weights = sorted->weights;
         if (y->type == MIXAQ_F32) return launch_linear<MIXAQ_F32, true>(A, form, codes.type, values, st);
