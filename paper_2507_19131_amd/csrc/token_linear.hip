@@ -344,6 +344,65 @@ struct SortedTiles {
 
 constexpr int GROUP_M = 4;                        // row tiles that run beside one another
 
+// The tile of this workgroup: TM rows from `first` to before `end`, of an expert, and its outputs' place tn; false where there is none.  A run of tiles
+// per XCD, so that what its CUs read at one time meets in its L2: in groups of GROUP_M row tiles with all their outputs, or row tile by row tile.
+template <int TM, bool SORTED>
+__device__ __forceinline__ bool tile_of(const TokenArgs& A, int tiles_m, int tiles_n, FastDiv by, int& tn, int& first, int& end, int& expert)
+{
+    SortedTiles<TM> sorted;
+    if (SORTED) sorted.count(A, tiles_m);
+    const int tiles = (SORTED ? sorted.total : tiles_m) * tiles_n, per_xcd = (tiles + 7) / 8;
+    const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per_xcd || t >= tiles) return false;
+    expert = 0;
+    if (SORTED) {
+        const int rt = by(t);
+        tn = t - rt * tiles_n;
+        sorted.find(A, rt, expert, first, end);
+    } else {
+        const int group = by(t), in = t - group * GROUP_M * tiles_n, gm = min(GROUP_M, tiles_m - group * GROUP_M);
+        tn = in / gm;
+        first = (group * GROUP_M + in - tn * gm) * TM;
+        end = min(A.M, first + TM);
+    }
+    return true;
+}
+
+// The sums of a wave's 32 MT rows from row0 on and of block nb, to results.
+template <int YT, int MT, bool SORTED>
+__device__ __forceinline__ void finish(const TokenArgs& A, const v16i (&acc)[MT][4], int expert, int nb, int row0, int end, v4i* turn)
+{
+    const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
+    const float* const sw = A.sw + ((long long)expert * A.NB + nb) * SBLOCK;
+    const float* const bias = A.bias + ((long long)expert * A.NB + nb) * SBLOCK;
+    float s[64], b[64];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __builtin_memcpy(&s[i * 16], sw + run_of(i, h), 64);
+        __builtin_memcpy(&b[i * 16], bias + run_of(i, h), 64);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int r = row0 + m * 32 + j, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
+        const float sx = A.sx[max(src, 0)];
+        float v[64];
+#pragma unroll
+        for (int T = 0; T < 4; ++T)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int to = place_of(T, e);
+                v[to] = fmaf((float)acc[m][T][e], sx * s[to], b[to]);
+            }
+        activate(v, A.act);
+        if (SORTED && A.weights) {
+            const float weight = A.weights[at];
+#pragma unroll
+            for (int e = 0; e < 64; ++e) v[e] *= weight;
+        }
+        store_rows<YT>(A, v, nb, row0 + m * 32, (unsigned)__ballot(r < end && src >= 0), turn);
+    }
+}
+
 // Waits until of the stages that this wave has requested, R loads each, at most min(CAP, left) are on their way.
 template <int R, int CAP>
 __device__ __forceinline__ void wait_stages(int left)
@@ -370,24 +429,8 @@ __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kern
     __shared__ v4i xs[RING][XP * 64], ws[RING][WP * 64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
     const int wm = wave / WN, wn = wave % WN, KB = A.KB, stages = (A.K + DEPTH - 1) / DEPTH;
-    // a run of tiles per XCD, so that what its CUs read at one time meets in its L2: in groups of GROUP_M row tiles with all their outputs, or row
-    // tile by row tile
-    SortedTiles<TM> sorted;
-    if (SORTED) sorted.count(A, tiles_m);
-    const int tiles = (SORTED ? sorted.total : tiles_m) * tiles_n, per_xcd = (tiles + 7) / 8;
-    const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per_xcd || t >= tiles) return;             // the whole workgroup
-    int tn, first, end, expert = 0;
-    if (SORTED) {
-        const int rt = by(t);
-        tn = t - rt * tiles_n;
-        sorted.find(A, rt, expert, first, end);
-    } else {
-        const int group = by(t), in = t - group * GROUP_M * tiles_n, gm = min(GROUP_M, tiles_m - group * GROUP_M);
-        tn = in / gm;
-        first = (group * GROUP_M + in - tn * gm) * TM;
-        end = min(A.M, first + TM);
-    }
+    int tn, first, end, expert;
+    if (!tile_of<TM, SORTED>(A, tiles_m, tiles_n, by, tn, first, end, expert)) return;       // the whole workgroup
     const int nb0 = tn * WN, nb = nb0 + wn;
 
     // what this wave requests: rows (wave XL + i) 16 + lane / 4 of x, whose lanes take the chunk that belongs in their place, and pieces wave WL + i of w
@@ -465,35 +508,84 @@ __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kern
     meet();
     if (nb >= A.NB) return;
     static_assert(RING * XP * 64 >= W * 512, "room for a wave's 32 rows of 256 bytes");
-    v4i* const turn = &xs[0][0] + wave * 512;
-    const float* const sw = A.sw + ((long long)expert * A.NB + nb) * SBLOCK;
-    const float* const bias = A.bias + ((long long)expert * A.NB + nb) * SBLOCK;
-    float s[64], b[64];
+    finish<YT, MT, SORTED>(A, acc, expert, nb, first + m0, end, &xs[0][0] + wave * 512);
+}
+
+// ---- weights straight from memory, x through LDS ------------------------------------------------------------------------------
+// Four waves, two by two, 128 rows and 128 outputs each.  With both operands in LDS its reads (64 KB a step of 64) and its direct loads (32 KB) take as
+// long as the matrix instructions.  Packed weights lie as the instruction takes them, so a wave loads its own into registers, four steps ahead.
+template <int YT, bool SORTED>
+__global__ __launch_bounds__(256, 1) void token_large_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
+{
+    constexpr int MT = 4, TM = 256, XP = 32, XL = 8, LARGE_RING = 2;         // 1 KB pieces of a stage of 128, a wave's
+    __shared__ v4i xs[LARGE_RING][XP * 64];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
+    const int wm = wave >> 1, wn = wave & 1, KB = A.KB;
+    int tn, first, end, expert;
+    if (!tile_of<TM, SORTED>(A, tiles_m, tiles_n, by, tn, first, end, expert)) return;       // the whole workgroup
+    const int nb = min(tn * 2 + wn, A.NB - 1);                               // (a wave without outputs computes its neighbour's and stores none)
+
+    // rows (wave XL + i) 8 + lane / 8 of x, whose lanes take the chunk that belongs in their place
+    const int chunk[2] = {((lane & 7) ^ (lane >> 4)) * 16, ((lane & 7) ^ (lane >> 4) ^ 4) * 16}, last_chunk = (A.K - 1) & ~15;      // of even and of odd pieces
+    const uint8_t* const xb = (const uint8_t*)A.x + (SORTED ? 0 : (long long)first * A.ldx);
+    unsigned from[XL];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        __builtin_memcpy(&s[i * 16], sw + run_of(i, h), 64);
-        __builtin_memcpy(&b[i * 16], bias + run_of(i, h), 64);
+    for (int i = 0; i < XL; ++i) {
+        const int r = min(first + (wave * XL + i) * 8 + (lane >> 3), end - 1);
+        from[i] = (unsigned)(SORTED ? max(source_of(A, r), 0) : r - first) * (unsigned)A.ldx;
     }
+    const unsigned lx = lds_address(xs);
+    auto request = [&](int kb, int i) {                                      // two pieces; behind a row's end the last chunk again, the weights there are zero
+        request2(xb, from[i] + min(kb * SBLOCK + chunk[0], last_chunk), from[i + 1] + min(kb * SBLOCK + chunk[1], last_chunk),
+                 lx + (kb % LARGE_RING * XP + wave * XL + i) * 1024, kb, KB);
+    };
+    auto meet = [] {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    const v4i* const wb = (const v4i*)(A.w + ((long long)expert * A.NB + nb) * KB * (8 * TILE_BYTES)) + (j >> 4) * 128 + h * 16 + (j & 15);
+    const int m0 = wm * 32 * MT;
+    v16i acc[MT][4] = {};
+    v4i x[2][MT], w[4][4];
+    auto load = [&](int kb, int c, int T) { w[c][T] = wb[(long long)min(kb, KB - 1) * 1024 + T * 256 + (c >> 1) * 64 + (c & 1) * 32]; };
+    const v4i* const xr = &xs[0][(m0 + j) * 8];
+    auto read = [&](int kb, int c, int i) { x[c & 1][i] = xr[kb % LARGE_RING * (XP * 64) + i * 256 + ((2 * c + h) ^ (j >> 1 & 7))]; };
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int row0 = first + m0 + m * 32, r = row0 + j, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
-        const float sx = A.sx[max(src, 0)];
-        float v[64];
+    for (int kb = 0; kb < LARGE_RING; ++kb)
 #pragma unroll
-        for (int T = 0; T < 4; ++T)
+        for (int i = 0; i < XL; i += 2) request(kb, i);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int to = place_of(T, e);
-                v[to] = fmaf((float)acc[m][T][e], sx * s[to], b[to]);
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int T = 0; T < 4; ++T) load(0, c, T);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    meet();
+#pragma unroll
+    for (int i = 0; i < MT; ++i) read(0, 0, i);
+#pragma unroll 1
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (c == 3) {                                                    // behind the last requests there are this stage's twelve loads of weights
+                asm volatile("s_waitcnt lgkmcnt(0) vmcnt(12)" ::: "memory");
+                meet();
             }
-        activate(v, A.act);
-        if (SORTED && A.weights) {
-            const float weight = A.weights[at];
 #pragma unroll
-            for (int e = 0; e < 64; ++e) v[e] *= weight;
+            for (int p = 0; p < 16; ++p) {
+                const int T = p / MT, m = p % MT;
+                __builtin_amdgcn_sched_barrier(0);
+                acc[m][T] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c][T], x[c & 1][m], acc[m][T], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (m == 3) load(kb + 1, c, T);
+                if (p < MT) read(c == 3 ? kb + 1 : kb, (c + 1) & 3, p);
+                if (c == 3 && m == 1) request(kb + LARGE_RING, T * 2);
+            }
         }
-        store_rows<YT>(A, v, nb, row0, (unsigned)__ballot(r < end && src >= 0), turn);
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");              // (and the last reads for nobody)
+    meet();
+    if (tn * 2 + wn >= A.NB) return;
+    finish<YT, MT, SORTED>(A, acc, expert, nb, first + m0, end, &xs[0][0] + wave * 512);
 }
 
 // Quantizes x first where it is given as values; behind the checks of the product that follows.
@@ -527,8 +619,9 @@ int launch_tiles(const TokenArgs& A, const mixaq_rows* values, hipStream_t st)
     if (blocks * WM * WN * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
     const int rc = quantize_first(A, values, st);
     if (rc) return rc;
-    hipLaunchKernelGGL((token_tile_kernel<YT, MT, WM, WN, SORTED>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, (int)tiles_m, tiles_n,
-                       FastDiv(SORTED ? tiles_n : GROUP_M * tiles_n));
+    const FastDiv by(SORTED ? tiles_n : GROUP_M * tiles_n);
+    if constexpr (MT == 4) hipLaunchKernelGGL((token_large_kernel<YT, SORTED>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, (int)tiles_m, tiles_n, by);
+    else hipLaunchKernelGGL((token_tile_kernel<YT, MT, WM, WN, SORTED>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, (int)tiles_m, tiles_n, by);
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
 }
