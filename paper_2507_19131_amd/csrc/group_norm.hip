@@ -28,12 +28,178 @@ struct GroupArgs {
     float* pivots;                    // [images][groups]: x may be written over
 };
 
-__device__ __forceinline__ double shfl_xor64(double v, int d)
+__device__ __forceinline__ double shfl64(double v, int from)
 {
     const long long b = __double_as_longlong(v);
-    const unsigned lo = (unsigned)__shfl_xor((int)b, d, 64), hi = (unsigned)__shfl_xor((int)(b >> 32), d, 64);
+    const unsigned lo = (unsigned)__shfl((int)b, from, 64), hi = (unsigned)__shfl((int)(b >> 32), from, 64);
     return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
+
+// Which rows and channels a thread takes: of up to 64 units a wave takes whole rows, 64 / units of them, of more the workgroup does.  slot < slots for threads that
+// take any; `left`: how many rows of sums there are once a wave has added up its own.
+struct Place { int u, slot, slots, of_wave, left; };
+__device__ __forceinline__ Place place_of(int units)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Place p;
+    if (units <= 64) {
+        p.of_wave = 64 / units;
+        const int s = lane / units;
+        p.u = lane - s * units;
+        p.slots = p.of_wave * (THREADS / 64);
+        p.slot = s < p.of_wave ? wave * p.of_wave + s : p.slots;
+        p.left = THREADS / 64;
+    } else {
+        p.of_wave = 1;
+        p.slots = p.left = THREADS / units;
+        p.slot = threadIdx.x / units;
+        p.u = threadIdx.x - p.slot * units;
+    }
+    return p;
+}
+
+// Adds up what the threads of a workgroup have for each group, of a unit's eight channels together (WHOLE) or each for itself: the rows of a wave by halves, then 16 lanes a
+// group the rows that are left.  One thread a group calls to(g, sums).  The order goes by the sizes alone.
+template <bool TINY, bool WHOLE, int E, typename To>
+__device__ __forceinline__ void add_up(double (&v)[E], double (&q)[E], const Place& p, int units, int per_group, int groups, int C, Sums (*red)[THREADS], To to)
+{
+    const int lane = threadIdx.x & 63;
+    for (int n = p.of_wave; n > 1;) {                                        // (lanes without a row hold zeros and are nobody's upper half)
+        const int half = (n + 1) / 2, from = lane + half * units, upper = from < n * units;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const double ov = shfl64(v[e], from), oq = shfl64(q[e], from);
+            v[e] += upper ? ov : 0.0;
+            q[e] += upper ? oq : 0.0;
+        }
+        n = half;
+    }
+    const int row = units <= 64 ? threadIdx.x >> 6 : p.slot;
+    if (p.slot < p.slots && (units > 64 || lane < units)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) red[e][row * units + p.u] = {v[e], q[e]};
+    }
+    __syncthreads();
+    for (int g0 = 0; g0 < groups; g0 += THREADS / 16) {
+        const int g = g0 + threadIdx.x / 16, l = threadIdx.x & 15;
+        Sums s = {0.0, 0.0};
+        if (g < groups && l < p.left) {
+            auto more = [&](const Sums& o) {
+                s.v += o.v;
+                s.q += o.q;
+            };
+            if constexpr (WHOLE) {
+                for (int i = g * (per_group / 8); i < (g + 1) * (per_group / 8); ++i) more(red[0][l * units + i]);
+            } else {
+                for (int i = g * per_group; i < (g + 1) * per_group; ++i) {
+                    const int unit = i / 8, at = place8<TINY>(unit * 8, C).at;
+                    more(red[i - at][l * units + unit]);
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            s.v += shfl64(s.v, lane ^ d);
+            s.q += shfl64(s.q, lane ^ d);
+        }
+        if (g < groups && l == 0) to(g, s);
+    }
+}
+template <bool WHOLE, int E>
+__device__ __forceinline__ void add(double (&v)[E], double (&q)[E], const float (&x)[8], const double (&pivot)[E])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const double d = (double)x[e] - pivot[WHOLE ? 0 : e];
+        v[WHOLE ? 0 : e] += d;
+        q[WHOLE ? 0 : e] = fma(d, d, q[WHOLE ? 0 : e]);
+    }
+}
+
+// What becomes of a group's values: (x - hi) a + b, a = r gamma, b = beta - lo a; hi + lo is the mean.
+struct Factors { float hi, lo, r; };
+__device__ __forceinline__ Factors factors_of(Sums s, double count, float pivot, float eps)
+{
+    const double n = 1.0 / count, off = s.v * n, mean = (double)pivot + off, variance = s.q * n - off * off;
+    Factors f;
+    f.hi = (float)mean;
+    f.lo = (float)(mean - (double)f.hi);
+    f.r = (float)(1.0 / sqrt((variance < 0.0 ? 0.0 : variance) + (double)eps));          // (a NaN stays one)
+    return f;
+}
+__device__ __forceinline__ void coefficients(const GroupArgs& A, Eight c, const Factors* of, int first, float (&hi)[8], float (&a)[8], float (&b)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int channel = min(c.at + e, A.C - 1);
+        const Factors f = of[channel / A.per_group - first];
+        hi[e] = f.hi;
+        a[e] = f.r * (A.gamma ? A.gamma[channel] : 1.0f);
+        b[e] = fmaf(-f.lo, a[e], A.beta ? A.beta[channel] : 0.0f);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void apply(const T (&x)[8], const float (&hi)[8], const float (&a)[8], const float (&b)[8], int act, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fmaf((float)x[e] - hi[e], a[e], b[e]);
+    activate(v, act);
+}
+template <bool TINY>
+__device__ __forceinline__ void store_values(const GroupArgs& A, long long row, Eight c, const float (&v)[8])
+{
+    if (A.y_type == MIXAQ_F32) store8<TINY>((float*)A.y + row * A.ldy, c, A.C, v);
+    else if (A.y_type == MIXAQ_F16) store8<TINY>((_Float16*)A.y + row * A.ldy, c, A.C, v);
+    else store8<TINY>((__bf16*)A.y + row * A.ldy, c, A.C, v);
+}
+
+// Small maps in one kernel: a workgroup holds its channels of an image, whole groups and whole units, in registers.
+constexpr int HELD = 4;                           // rows of a thread
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int parts)
+{
+    constexpr int E = WHOLE ? 1 : 8;
+    __shared__ Sums red[E][THREADS];
+    __shared__ Factors factor[8];                                            // (of lcm(8, per_group) channels)
+    const int image = blockIdx.x / parts, part = blockIdx.x - image * parts, width = A.C / parts, units = width / 8;
+    const Place p = place_of(units);
+    const int slots = p.slots, slot = p.slot, first = part * width / A.per_group;
+    const Eight c = {part * width + p.u * 8, 0};
+    const T* const map = (const T*)A.x + (long long)image * A.rows * A.ldx;
+    T x[HELD][8];
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) load8<false>(map + (long long)min(slot + k * slots, A.rows - 1) * A.ldx, c, A.C, x[k]);
+    double pivot[E], v[E] = {}, q[E] = {};
+#pragma unroll
+    for (int e = 0; e < E; ++e) pivot[e] = (double)(float)map[(c.at + e) / A.per_group * A.per_group];
+    const float mine = (float)map[(first + min((int)threadIdx.x, width / A.per_group - 1)) * A.per_group];         // the pivot of group threadIdx.x
+    __shared__ float pivots[8];
+    if (threadIdx.x < 8) pivots[threadIdx.x] = mine;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+        if (slot < slots && slot + k * slots < A.rows) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = (float)x[k][e];
+            add<WHOLE>(v, q, f, pivot);
+        }
+    add_up<false, WHOLE>(v, q, p, units, A.per_group, width / A.per_group, width, red, [&](int g, Sums s) {
+        factor[g] = factors_of(s, (double)A.rows * A.per_group, pivots[g], A.eps);
+    });
+    __syncthreads();                                                         // (every value has been read: y may be x)
+    float hi[8], a[8], b[8];
+    coefficients(A, c, factor, first, hi, a, b);
+    if (slot >= slots) return;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+        if (slot + k * slots >= A.rows) break;
+        float f[8];
+        apply(x[k], hi, a, b, A.act, f);
+        store_values<false>(A, (long long)image * A.rows + slot + k * slots, c, f);
+    }
+}
+
+constexpr int AHEAD = 4;                          // rows of a thread that are on their way at one time
 
 // The sums of one chunk of rows.  A thread keeps to eight channels, so that the threads of a workgroup read whole rows one behind the other.  WHOLE: a
 // group is a multiple of eight channels, whose sums a thread takes together.
@@ -41,145 +207,130 @@ template <typename T, bool TINY, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void group_sums_kernel(GroupArgs A)
 {
     constexpr int E = WHOLE ? 1 : 8;
-    __shared__ double red[E][THREADS];
+    __shared__ Sums red[E][THREADS];
     const int image = blockIdx.x / A.chunks, chunk = blockIdx.x - image * A.chunks;
-    const int slots = THREADS / A.units, slot = threadIdx.x / A.units, u = threadIdx.x - slot * A.units;
-    const Eight c = place8<TINY>(u * 8, A.C);
+    const Place p = place_of(A.units);
+    const int slots = p.slots, slot = p.slot;
+    const Eight c = place8<TINY>(p.u * 8, A.C);
     const T* const map = (const T*)A.x + (long long)image * A.rows * A.ldx;
     double pivot[E], v[E] = {}, q[E] = {};
 #pragma unroll
     for (int e = 0; e < E; ++e) pivot[e] = (double)(float)map[min(c.at + e, A.C - 1) / A.per_group * A.per_group];
     if (slot < slots) {
         const int end = min((chunk + 1) * A.chunk_rows, A.rows);
-        for (int r = chunk * A.chunk_rows + slot; r < end; r += slots) {
-            float x[8];
-            load8f<TINY>(map + (long long)r * A.ldx, c, A.C, x);
+        int r = chunk * A.chunk_rows + slot;
+        for (; r + (AHEAD - 1) * slots < end; r += AHEAD * slots) {
+            T x[AHEAD][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double d = (double)x[e] - pivot[WHOLE ? 0 : e];
-                v[WHOLE ? 0 : e] += d;
-                q[WHOLE ? 0 : e] = fma(d, d, q[WHOLE ? 0 : e]);
+            for (int k = 0; k < AHEAD; ++k) load8<TINY>(map + (long long)(r + k * slots) * A.ldx, c, A.C, x[k]);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = (float)x[k][e];
+                add<WHOLE>(v, q, f, pivot);
             }
         }
-    }
-    // a group's lanes: a power of two, with about eight values each
-    const int per = WHOLE ? A.per_group / 8 : A.per_group, count = slots * per;
-    int lanes = 1;
-    while (lanes < 64 && lanes * 8 < count) lanes *= 2;
-    double total[2];
-    for (int round = 0; round * (THREADS / lanes) < A.groups; ++round) {
-        const int g = round * (THREADS / lanes) + threadIdx.x / lanes, l = threadIdx.x % lanes;
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            __syncthreads();                                                 // (one kind of sums at a time lies in LDS)
-#pragma unroll
-            for (int e = 0; e < E; ++e) red[e][threadIdx.x] = which ? q[e] : v[e];
-            __syncthreads();
-            double s = 0.0;
-            if (g < A.groups)
-                for (int i = l; i < count; i += lanes) {
-                    const int at = i / per, channel = g * per + i - at * per;            // (WHOLE: unit)
-                    if constexpr (WHOLE) s += red[0][at * A.units + channel];
-                    else {
-                        const int unit = channel / 8, from = place8<TINY>(unit * 8, A.C).at;
-                        s += red[channel - from][at * A.units + unit];
-                    }
-                }
-            for (int d = 1; d < lanes; d <<= 1) s += shfl_xor64(s, d);
-            total[which] = s;
-        }
-        if (g < A.groups && l == 0) {
-            A.part[((long long)image * A.chunks + chunk) * A.groups + g] = {total[0], total[1]};
-            if (chunk == 0) A.pivots[(long long)image * A.groups + g] = (float)map[g * A.per_group];
+        for (; r < end; r += slots) {
+            float f[8];
+            load8f<TINY>(map + (long long)r * A.ldx, c, A.C, f);
+            add<WHOLE>(v, q, f, pivot);
         }
     }
+    add_up<TINY, WHOLE>(v, q, p, A.units, A.per_group, A.groups, A.C, red, [&](int g, Sums s) {
+        A.part[((long long)image * A.chunks + chunk) * A.groups + g] = s;
+        if (chunk == 0) A.pivots[(long long)image * A.groups + g] = (float)map[g * A.per_group];
+    });
 }
 
-// Chunk by chunk again: every workgroup adds up its image's sums first, in the order of the chunks.  `lanes` lanes a row: for values as many as it has units of
-// eight channels, for codes a power of two, whose maximum goes through the lanes and, of more than a wave, through LDS.
+// Chunk by chunk again, from its last rows, which the caches are likely to hold, to the first: every workgroup adds up its image's sums first, in an order that goes
+// by the sizes alone, while its first rows are on their way.  `lanes` lanes a row: for values as many as it has units of eight channels, for codes a power of
+// two, whose maximum goes through the lanes and, of more than a wave, through LDS.
 template <typename T, bool TINY>
 __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
 {
-    __shared__ float mean_hi[MOST_GROUPS], mean_lo[MOST_GROUPS], factor[MOST_GROUPS];
+    constexpr int TURN = sizeof(T) == 4 ? AHEAD / 2 : AHEAD;
+    __shared__ Sums merge[THREADS];
+    __shared__ Factors factor[MOST_GROUPS];
     __shared__ unsigned part[2][THREADS / 64];
     const int image = blockIdx.x / A.chunks, chunk = blockIdx.x - image * A.chunks;
     const T* const map = (const T*)A.x + (long long)image * A.rows * A.ldx;
-    {
-        int lanes = 1;                                                       // of a group
-        while (lanes < 64 && lanes * 2 <= A.chunks && lanes * 2 * A.groups <= THREADS) lanes *= 2;
-        for (int g0 = 0; g0 < A.groups; g0 += THREADS / lanes) {
-            const int g = g0 + threadIdx.x / lanes, l = threadIdx.x % lanes;
-            double v = 0.0, q = 0.0;
-            if (g < A.groups)
-                for (int i = l; i < A.chunks; i += lanes) {
-                    const Sums s = A.part[((long long)image * A.chunks + i) * A.groups + g];
-                    v += s.v;
-                    q += s.q;
-                }
-            for (int d = 1; d < lanes; d <<= 1) {
-                v += shfl_xor64(v, d);
-                q += shfl_xor64(q, d);
-            }
-            if (g < A.groups && l == 0) {
-                const double n = 1.0 / ((double)A.rows * A.per_group), off = v * n, mean = (double)A.pivots[(long long)image * A.groups + g] + off;
-                const double variance = q * n - off * off;
-                mean_hi[g] = (float)mean;
-                mean_lo[g] = (float)(mean - (double)mean_hi[g]);
-                factor[g] = (float)(1.0 / sqrt((variance < 0.0 ? 0.0 : variance) + (double)A.eps));        // (a NaN stays one)
-            }
-        }
-    }
-    __syncthreads();
     const int slots = THREADS / A.lanes, slot = threadIdx.x / A.lanes, u = threadIdx.x - slot * A.lanes;
     const Eight c = place8<TINY>(u * 8, A.C);
-    float hi[8], a[8], b[8];                                                 // y = (x - hi) a + b
+    const int first = chunk * A.chunk_rows, end = min(first + A.chunk_rows, A.rows), step = TURN * slots;
+    T x[TURN][8];
+    auto row_of = [&](int r0, int k) { return r0 + k * slots + slot; };
+    auto request = [&](int r0) {                                             // (spare lanes take the last row along)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int channel = min(c.at + e, A.C - 1), g = channel / A.per_group;
-        hi[e] = mean_hi[g];
-        a[e] = factor[g] * (A.gamma ? A.gamma[channel] : 1.0f);
-        b[e] = fmaf(-mean_lo[g], a[e], A.beta ? A.beta[channel] : 0.0f);
-    }
-    const int end = min((chunk + 1) * A.chunk_rows, A.rows);
-    int turn = 0;
-    for (int r0 = chunk * A.chunk_rows; r0 < end; r0 += slots) {
-        const bool real = slot < slots && r0 + slot < end;
-        const int r = min(r0 + slot, end - 1);
-        float v[8];
-        load8f<TINY>(map + (long long)r * A.ldx, c, A.C, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e] - hi[e], a[e], b[e]);
-        activate(v, A.act);
-        const long long row = (long long)image * A.rows + r;
-        if (A.y_type == MIXAQ_I8) {
-            unsigned m = max_magnitude<TINY>(c, A.C, v);
-            for (int d = 1; d < A.lanes && d < 64; d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
-            if (A.lanes > 64) {                                              // (two places in turn: who writes one again has passed the other's barrier)
-                if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = m;
-                __syncthreads();
-                const int first = slot * (A.lanes / 64);
-                for (int w = 0; w < A.lanes / 64; ++w) m = max(m, part[turn][first + w]);
-                turn ^= 1;
+        for (int k = 0; k < TURN; ++k) load8<TINY>(map + (long long)min(row_of(r0, k), end - 1) * A.ldx, c, A.C, x[k]);
+    };
+    int r0 = first + (end - 1 - first) / step * step;
+    request(r0);
+    {
+        const int teams = THREADS / A.groups, g = threadIdx.x % A.groups, l = threadIdx.x / A.groups;
+        int fold = 1;                                                        // the largest power of two up to teams and chunks
+        while (fold * 2 <= teams && fold * 2 <= A.chunks) fold *= 2;
+        if (l < fold) {
+            Sums s = {0.0, 0.0};
+            for (int i = l; i < A.chunks; i += fold) {
+                const Sums o = A.part[((long long)image * A.chunks + i) * A.groups + g];
+                s.v += o.v;
+                s.q += o.q;
             }
-            const RowScale s = row_scale(m);
-            if (real) {
-                store_int_codes8<TINY>((int8_t*)A.y + row * A.ldy, c, A.C, v, s.inv);
-                if (u == 0) A.scales[row] = s.scale;
-            }
-        } else if (real) {
-            if (A.y_type == MIXAQ_F32) store8<TINY>((float*)A.y + row * A.ldy, c, A.C, v);
-            else if (A.y_type == MIXAQ_F16) store8<TINY>((_Float16*)A.y + row * A.ldy, c, A.C, v);
-            else store8<TINY>((__bf16*)A.y + row * A.ldy, c, A.C, v);
+            merge[threadIdx.x] = s;
         }
+        for (int d = fold / 2; d; d /= 2) {
+            __syncthreads();
+            if (l < d) {
+                merge[threadIdx.x].v += merge[threadIdx.x + d * A.groups].v;
+                merge[threadIdx.x].q += merge[threadIdx.x + d * A.groups].q;
+            }
+        }
+        if (l == 0) factor[g] = factors_of(merge[g], (double)A.rows * A.per_group, A.pivots[(long long)image * A.groups + g], A.eps);
+    }
+    __syncthreads();
+    float hi[8], a[8], b[8];
+    coefficients(A, c, factor, 0, hi, a, b);
+    int turn = 0;
+    for (;;) {
+        float v[TURN][8];
+#pragma unroll
+        for (int k = 0; k < TURN; ++k) apply(x[k], hi, a, b, A.act, v[k]);
+        const int now = r0;
+        r0 -= step;
+        if (r0 >= first) request(r0);
+#pragma unroll
+        for (int k = 0; k < TURN; ++k) {
+            const bool real = slot < slots && row_of(now, k) < end;
+            const long long row = (long long)image * A.rows + row_of(now, k);
+            if (A.y_type == MIXAQ_I8) {
+                unsigned m = max_magnitude<TINY>(c, A.C, v[k]);
+                for (int d = 1; d < A.lanes && d < 64; d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d, 64));
+                if (A.lanes > 64) {                                          // (two places in turn: who writes one again has passed the other's barrier)
+                    if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = m;
+                    __syncthreads();
+                    const int wave = slot * (A.lanes / 64);
+                    for (int w = 0; w < A.lanes / 64; ++w) m = max(m, part[turn][wave + w]);
+                    turn ^= 1;
+                }
+                const RowScale s = row_scale(m);
+                if (real) {
+                    store_int_codes8<TINY>((int8_t*)A.y + row * A.ldy, c, A.C, v[k], s.inv);
+                    if (u == 0) A.scales[row] = s.scale;
+                }
+            } else if (real) store_values<TINY>(A, row, c, v[k]);
+        }
+        if (r0 < first) break;
     }
 }
 
-// Chunks of an image: about two workgroups a CU in all, each with rows for several turns.
+// Chunks of an image: a workgroup a CU in all (what every one adds up first grows with their number), each with rows for a turn of AHEAD or more.
+int slots_of(int units) { return units <= 64 ? 64 / units * (THREADS / 64) : THREADS / units; }
 struct Chunks { int count, rows; };
 Chunks chunks_of(int rows, int images, int units)
 {
-    const int turn = THREADS / units;
-    const long long most = ((long long)rows + 4LL * turn - 1) / (4LL * turn), wanted = std::max(1, (512 + images - 1) / images);
+    const int turn = slots_of(units);
+    const long long most = ((long long)rows + AHEAD * turn - 1) / (AHEAD * turn), wanted = std::max(1, (256 + images - 1) / images);
     const int count = (int)std::min(most, wanted), per = (rows + count - 1) / count;
     return {(rows + per - 1) / per, per};
 }
@@ -207,6 +358,21 @@ size_t sums_bytes(const mixaq_group_norm_desc& d, int images)
 }
 size_t workspace_of(const mixaq_group_norm_desc& d, int images) { return images ? sums_bytes(d, images) + (size_t)images * d.groups * sizeof(float) : 0; }
 
+// Of how many parts an image's channels are, whole groups and whole units of eight each, where a workgroup holds the rows of one; 0 where none does.
+int parts_of(const mixaq_group_norm_desc& d)
+{
+    int width = d.C / d.groups;
+    while (width % 8) width += d.C / d.groups;                               // (after at most eight)
+    if (d.C % 8 || d.C % width || width / 8 > THREADS || (d.rows_per_image - 1LL) / slots_of(width / 8) >= HELD) return 0;
+    return d.C / width;
+}
+
+template <typename T>
+void launch_small(const GroupArgs& A, int parts, unsigned blocks, hipStream_t st)
+{
+    if (A.per_group % 8 == 0) hipLaunchKernelGGL((group_small_kernel<T, true>), dim3(blocks), dim3(THREADS), 0, st, A, parts);
+    else hipLaunchKernelGGL((group_small_kernel<T, false>), dim3(blocks), dim3(THREADS), 0, st, A, parts);
+}
 template <typename T, bool TINY>
 void launch(const GroupArgs& A, unsigned blocks, hipStream_t st)
 {
@@ -215,10 +381,11 @@ void launch(const GroupArgs& A, unsigned blocks, hipStream_t st)
     hipLaunchKernelGGL((group_norm_kernel<T, TINY>), dim3(blocks), dim3(THREADS), 0, st, A);
 }
 template <int TYPE>
-void launch_type(const GroupArgs& A, unsigned blocks, hipStream_t st)
+void launch_type(const GroupArgs& A, int parts, unsigned blocks, hipStream_t st)
 {
     using T = typename TypeOf<TYPE>::T;
-    if (A.C < 8) launch<T, true>(A, blocks, st);
+    if (parts) launch_small<T>(A, parts, blocks, st);
+    else if (A.C < 8) launch<T, true>(A, blocks, st);
     else launch<T, false>(A, blocks, st);
 }
 
@@ -278,11 +445,12 @@ int mixaq_group_norm(const mixaq_group_norm_desc* desc, const mixaq_group_norm_p
     A.gamma = params->gamma; A.beta = params->beta;
     A.part = (Sums*)workspace;
     A.pivots = (float*)((char*)workspace + sums_bytes(d, images));
-    const long long blocks = (long long)images * ch.count;
+    const int parts = y->type == MIXAQ_I8 ? 0 : parts_of(d);
+    const long long blocks = (long long)images * (parts ? parts : ch.count);
     if (blocks * THREADS >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d images are too many for one call", images);
-    if (x->type == MIXAQ_F32) launch_type<MIXAQ_F32>(A, (unsigned)blocks, (hipStream_t)stream);
-    else if (x->type == MIXAQ_F16) launch_type<MIXAQ_F16>(A, (unsigned)blocks, (hipStream_t)stream);
-    else launch_type<MIXAQ_BF16>(A, (unsigned)blocks, (hipStream_t)stream);
+    if (x->type == MIXAQ_F32) launch_type<MIXAQ_F32>(A, parts, (unsigned)blocks, (hipStream_t)stream);
+    else if (x->type == MIXAQ_F16) launch_type<MIXAQ_F16>(A, parts, (unsigned)blocks, (hipStream_t)stream);
+    else launch_type<MIXAQ_BF16>(A, parts, (unsigned)blocks, (hipStream_t)stream);
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
 }

@@ -4,7 +4,7 @@
 
 namespace mixaq {
 
-enum TokenForm { TOKEN_FEW, TOKEN_MID, TOKEN_SPLIT, TOKEN_TILE, TOKEN_LARGE };
+enum TokenForm { TOKEN_FEW, TOKEN_MID, TOKEN_SPLIT, TOKEN_TILE, TOKEN_WIDE, TOKEN_LARGE };
 
 // Whether values are quantized on their way into the product: every workgroup does it for its rows
 inline bool token_quantized_inside(int x_rows, int KB) { return x_rows <= 16; }

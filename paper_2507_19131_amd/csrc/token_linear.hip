@@ -251,32 +251,33 @@ __device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigne
 __device__ __forceinline__ int run_of(int i, int h) { return (i >> 1) * 64 + (2 * (i & 1) + h) * 16; }
 __device__ __forceinline__ constexpr int place_of(int T, int e) { return ((T >> 1) * 2 + (e >> 2 & 1)) * 16 + ((T & 1) * 2 + (e >> 3)) * 4 + (e & 3); }
 
-// The end of a wave's 32 rows and 128 outputs: a lane holds those of one row, in 4 runs of 16 neighbouring ones, the lanes l and l + 32 the whole row.  Through LDS
-// (`turn`: 32 rows x 256 bytes of the wave's own), so that a store covers whole lines; its 16-byte pieces are turned by the row, so that
-// neither side meets a bank twice.  kept: a bit for each row that is stored.
-template <int YT>
-__device__ __forceinline__ void store_rows(const TokenArgs& A, const float (&v)[64], int nb, int row0, unsigned kept, v4i* turn)
+// The end of a wave's 32 rows and 64 H outputs from n0 on: a lane holds those of one row, in 2 H runs of 16 neighbouring ones, the lanes l and l + 32 the whole row.
+// Through LDS (`turn`: 32 rows x 256 bytes of the wave's own, of which 64 outputs of 16 bits take half), so that a store covers whole lines; its 16-byte pieces
+// are turned by the row, so that neither side meets a bank twice.  kept: a bit for each row that is stored.
+template <int YT, int H>
+__device__ __forceinline__ void store_rows(const TokenArgs& A, const float (&v)[32 * H], int n0, int row0, unsigned kept, v4i* turn)
 {
     using T = typename TypeOf<YT>::T;
-    constexpr int ES = sizeof(T), PASSES = ES / 2;
+    constexpr int ES = sizeof(T), ROW_BYTES = 64 * H * ES < 256 ? 64 * H * ES : 256, PASSES = 64 * H * ES / ROW_BYTES, PIECES = ROW_BYTES / 16, RUNS = 2 * H / PASSES;
     const int lane = threadIdx.x & 63, own = lane & 31, h = lane >> 5;
     auto in_order = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };           // among the lanes of the wave, which runs in step
+    auto place = [](int r, int p) { return r * PIECES + (PIECES == 16 ? p ^ (r & 15) : p ^ (r >> 1 & 7)); };
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
 #pragma unroll
-        for (int i = pass * 4 / PASSES; i < (pass + 1) * 4 / PASSES; ++i) {
+        for (int i = pass * RUNS; i < (pass + 1) * RUNS; ++i) {
             T t[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) t[e] = (T)v[i * 16 + e];
-            const int p = run_of(i, h) * ES % 256 / 16;
+            const int p = run_of(i, h) * ES % ROW_BYTES / 16;
 #pragma unroll
-            for (int q = 0; q < ES; ++q) __builtin_memcpy(&turn[own * 16 + ((p + q) ^ (own & 15))], (const uint8_t*)t + q * 16, 16);
+            for (int q = 0; q < ES; ++q) __builtin_memcpy(&turn[place(own, p + q)], (const uint8_t*)t + q * 16, 16);
         }
         in_order();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int r = k * 4 + (lane >> 4), p = lane & 15, n = nb * SBLOCK + (pass * 256 + p * 16) / ES;
-            const v4i piece = turn[r * 16 + (p ^ (r & 15))];
+        for (int k = 0; k < PIECES / 2; ++k) {
+            const int r = (k * 64 + lane) / PIECES, p = lane % PIECES, n = n0 + (pass * ROW_BYTES + p * 16) / ES;
+            const v4i piece = turn[place(r, p)];
             if (!(kept >> r & 1)) continue;
             T* const to = (T*)A.y + (long long)(row0 + r) * A.ldy + n;
             if (n + 16 / ES <= A.N) __builtin_memcpy(to, &piece, 16);
@@ -368,26 +369,25 @@ __device__ __forceinline__ bool tile_of(const TokenArgs& A, int tiles_m, int til
     return true;
 }
 
-// The sums of a wave's 32 MT rows from row0 on and of block nb, to results.
-template <int YT, int MT, bool SORTED>
-__device__ __forceinline__ void finish(const TokenArgs& A, const v16i (&acc)[MT][4], int expert, int nb, int row0, int end, v4i* turn)
+// The sums of a wave's 32 MT rows from row0 on and of its 64 H outputs from n0 on, to results.
+template <int YT, int MT, int H, bool SORTED>
+__device__ __forceinline__ void finish(const TokenArgs& A, const v16i (&acc)[MT][2 * H], int expert, int n0, int row0, int end, v4i* turn)
 {
     const int lane = threadIdx.x & 63, j = lane & 31, h = lane >> 5;
-    const float* const sw = A.sw + ((long long)expert * A.NB + nb) * SBLOCK;
-    const float* const bias = A.bias + ((long long)expert * A.NB + nb) * SBLOCK;
-    float s[64], b[64];
+    const long long layer = (long long)expert * A.NB * SBLOCK + n0;
+    float s[32 * H], b[32 * H];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        __builtin_memcpy(&s[i * 16], sw + run_of(i, h), 64);
-        __builtin_memcpy(&b[i * 16], bias + run_of(i, h), 64);
+    for (int i = 0; i < 2 * H; ++i) {
+        __builtin_memcpy(&s[i * 16], A.sw + layer + run_of(i, h), 64);
+        __builtin_memcpy(&b[i * 16], A.bias + layer + run_of(i, h), 64);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int r = row0 + m * 32 + j, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
         const float sx = A.sx[max(src, 0)];
-        float v[64];
+        float v[32 * H];
 #pragma unroll
-        for (int T = 0; T < 4; ++T)
+        for (int T = 0; T < 2 * H; ++T)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int to = place_of(T, e);
@@ -397,9 +397,9 @@ __device__ __forceinline__ void finish(const TokenArgs& A, const v16i (&acc)[MT]
         if (SORTED && A.weights) {
             const float weight = A.weights[at];
 #pragma unroll
-            for (int e = 0; e < 64; ++e) v[e] *= weight;
+            for (int e = 0; e < 32 * H; ++e) v[e] *= weight;
         }
-        store_rows<YT>(A, v, nb, row0 + m * 32, (unsigned)__ballot(r < end && src >= 0), turn);
+        store_rows<YT, H>(A, v, n0, row0 + m * 32, (unsigned)__ballot(r < end && src >= 0), turn);
     }
 }
 
@@ -508,22 +508,21 @@ __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kern
     meet();
     if (nb >= A.NB) return;
     static_assert(RING * XP * 64 >= W * 512, "room for a wave's 32 rows of 256 bytes");
-    finish<YT, MT, SORTED>(A, acc, expert, nb, first + m0, end, &xs[0][0] + wave * 512);
+    finish<YT, MT, 2, SORTED>(A, acc, expert, nb * SBLOCK, first + m0, end, &xs[0][0] + wave * 512);
 }
 
 // ---- weights straight from memory, x through LDS ------------------------------------------------------------------------------
-// Four waves, two by two, 128 rows and 128 outputs each.  With both operands in LDS its reads (64 KB a step of 64) and its direct loads (32 KB) take as
-// long as the matrix instructions.  Packed weights lie as the instruction takes them, so a wave loads its own into registers, four steps ahead.
-template <int YT, bool SORTED>
-__global__ __launch_bounds__(256, 1) void token_large_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
+// Four waves side by side, all 32 MT rows and 64 outputs each.  Packed weights lie as the instruction takes them, so a wave loads its own into registers, four
+// steps ahead, and no weight comes twice; x goes through two LDS buffers of 128.
+template <int YT, int MT, bool SORTED>
+__global__ __launch_bounds__(256, MT == 2 ? 4 : 2) void token_wide_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
 {
-    constexpr int MT = 4, TM = 256, XP = 32, XL = 8, LARGE_RING = 2;         // 1 KB pieces of a stage of 128, a wave's
-    __shared__ v4i xs[LARGE_RING][XP * 64];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
-    const int wm = wave >> 1, wn = wave & 1, KB = A.KB;
+    constexpr int TM = 32 * MT, XP = TM / 8, XL = XP / 4;                    // 1 KB pieces of a stage, a wave's
+    __shared__ v4i xs[2][XP * 64];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5, KB = A.KB;
     int tn, first, end, expert;
     if (!tile_of<TM, SORTED>(A, tiles_m, tiles_n, by, tn, first, end, expert)) return;       // the whole workgroup
-    const int nb = min(tn * 2 + wn, A.NB - 1);                               // (a wave without outputs computes its neighbour's and stores none)
+    const int n0 = tn * 256 + wave * 64, nb = min(n0 / SBLOCK, A.NB - 1);    // (a wave without outputs computes others' and stores none)
 
     // rows (wave XL + i) 8 + lane / 8 of x, whose lanes take the chunk that belongs in their place
     const int chunk[2] = {((lane & 7) ^ (lane >> 4)) * 16, ((lane & 7) ^ (lane >> 4) ^ 4) * 16}, last_chunk = (A.K - 1) & ~15;      // of even and of odd pieces
@@ -537,55 +536,56 @@ __global__ __launch_bounds__(256, 1) void token_large_kernel(TokenArgs A, int ti
     const unsigned lx = lds_address(xs);
     auto request = [&](int kb, int i) {                                      // two pieces; behind a row's end the last chunk again, the weights there are zero
         request2(xb, from[i] + min(kb * SBLOCK + chunk[0], last_chunk), from[i + 1] + min(kb * SBLOCK + chunk[1], last_chunk),
-                 lx + (kb % LARGE_RING * XP + wave * XL + i) * 1024, kb, KB);
+                 lx + ((kb & 1) * XP + wave * XL + i) * 1024, kb, KB);
     };
     auto meet = [] {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    const v4i* const wb = (const v4i*)(A.w + ((long long)expert * A.NB + nb) * KB * (8 * TILE_BYTES)) + (j >> 4) * 128 + h * 16 + (j & 15);
-    const int m0 = wm * 32 * MT;
-    v16i acc[MT][4] = {};
-    v4i x[2][MT], w[4][4];
+    const v4i* const wb = (const v4i*)(A.w + (((long long)expert * A.NB + nb) * KB * 8 + (n0 % SBLOCK ? 4 : 0)) * TILE_BYTES) + (j >> 4) * 128 + h * 16 + (j & 15);
+    v16i acc[MT][2] = {};
+    v4i x[2][MT], w[4][2];
     auto load = [&](int kb, int c, int T) { w[c][T] = wb[(long long)min(kb, KB - 1) * 1024 + T * 256 + (c >> 1) * 64 + (c & 1) * 32]; };
-    const v4i* const xr = &xs[0][(m0 + j) * 8];
-    auto read = [&](int kb, int c, int i) { x[c & 1][i] = xr[kb % LARGE_RING * (XP * 64) + i * 256 + ((2 * c + h) ^ (j >> 1 & 7))]; };
+    const v4i* const xr = &xs[0][j * 8];
+    auto read = [&](int kb, int c, int i) { x[c & 1][i] = xr[(kb & 1) * (XP * 64) + i * 256 + ((2 * c + h) ^ (j >> 1 & 7))]; };
 #pragma unroll
-    for (int kb = 0; kb < LARGE_RING; ++kb)
-#pragma unroll
-        for (int i = 0; i < XL; i += 2) request(kb, i);
+    for (int i = 0; i < XL; i += 2) request(0, i);
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int T = 0; T < 4; ++T) load(0, c, T);
+        for (int T = 0; T < 2; ++T) load(0, c, T);
+#pragma unroll
+    for (int i = 0; i < XL; i += 2) request(1, i);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     meet();
 #pragma unroll
     for (int i = 0; i < MT; ++i) read(0, 0, i);
+    // Of each stage four steps of 32.  What a step's products need of x is read under those of the step before; behind the last read of a stage the waves
+    // meet, and its buffer is requested anew.  The last stage reads on like the others, for nobody.
 #pragma unroll 1
     for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            if (c == 3) {                                                    // behind the last requests there are this stage's twelve loads of weights
-                asm volatile("s_waitcnt lgkmcnt(0) vmcnt(12)" ::: "memory");
+            if (c == 3) {                                                    // behind the last requests there are this stage's six loads of weights
+                asm volatile("s_waitcnt lgkmcnt(0) vmcnt(6)" ::: "memory");
                 meet();
             }
 #pragma unroll
-            for (int p = 0; p < 16; ++p) {
+            for (int p = 0; p < 2 * MT; ++p) {
                 const int T = p / MT, m = p % MT;
                 __builtin_amdgcn_sched_barrier(0);
                 acc[m][T] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c][T], x[c & 1][m], acc[m][T], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                if (m == 3) load(kb + 1, c, T);
+                if (m == MT - 1) load(kb + 1, c, T);
                 if (p < MT) read(c == 3 ? kb + 1 : kb, (c + 1) & 3, p);
-                if (c == 3 && m == 1) request(kb + LARGE_RING, T * 2);
+                if (c == 3 && p % 2 == 1 && p < XL + (XL == 2)) request(kb + 2, p - 1);
             }
         }
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");              // (and the last reads for nobody)
     meet();
-    if (tn * 2 + wn >= A.NB) return;
-    finish<YT, MT, SORTED>(A, acc, expert, nb, first + m0, end, &xs[0][0] + wave * 512);
+    if (n0 >= A.N) return;
+    finish<YT, MT, 1, SORTED>(A, acc, expert, n0, first, end, &xs[0][0] + wave * 512);
 }
 
 // Quantizes x first where it is given as values; behind the checks of the product that follows.
@@ -609,19 +609,18 @@ int launch_few(const TokenArgs& A, const mixaq_rows* values, hipStream_t st)
     return MIXAQ_OK;
 }
 
-template <int YT, int MT, int WM, int WN, bool SORTED>
+template <int YT, int TM, int TN, bool SORTED>
 int launch_tiles(const TokenArgs& A, const mixaq_rows* values, hipStream_t st)
 {
-    constexpr int TM = 32 * MT * WM;
-    const int tiles_n = (A.NB + WN - 1) / WN;
+    const int tiles_n = (A.NB + TN / SBLOCK - 1) / (TN / SBLOCK);
     const long long tiles_m = ((long long)A.M + TM - 1) / TM + (SORTED ? std::min(A.experts, A.M) : 0);      // (every expert's last tile may be cut)
     const long long blocks = (tiles_m * tiles_n + 7) / 8 * 8;
-    if (blocks * WM * WN * 64 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
+    if (blocks * 256 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d rows of %d outputs are too many for one call", A.M, A.N);
     const int rc = quantize_first(A, values, st);
     if (rc) return rc;
     const FastDiv by(SORTED ? tiles_n : GROUP_M * tiles_n);
-    if constexpr (MT == 4) hipLaunchKernelGGL((token_large_kernel<YT, SORTED>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, (int)tiles_m, tiles_n, by);
-    else hipLaunchKernelGGL((token_tile_kernel<YT, MT, WM, WN, SORTED>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0, st, A, (int)tiles_m, tiles_n, by);
+    if constexpr (TN == 256) hipLaunchKernelGGL((token_wide_kernel<YT, TM / 32, SORTED>), dim3((unsigned)blocks), dim3(256), 0, st, A, (int)tiles_m, tiles_n, by);
+    else hipLaunchKernelGGL((token_tile_kernel<YT, TM / 128, 4, 1, SORTED>), dim3((unsigned)blocks), dim3(256), 0, st, A, (int)tiles_m, tiles_n, by);
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
 }
@@ -630,8 +629,9 @@ template <int YT, bool SORTED>
 int launch_linear(const TokenArgs& A, TokenForm form, int x_type, const mixaq_rows* values, hipStream_t st)
 {
     switch (form) {
-    case TOKEN_TILE: return launch_tiles<YT, 1, 4, 1, SORTED>(A, values, st);
-    case TOKEN_LARGE: return launch_tiles<YT, 4, 2, 2, SORTED>(A, values, st);
+    case TOKEN_TILE: return launch_tiles<YT, 128, 128, SORTED>(A, values, st);
+    case TOKEN_WIDE: return launch_tiles<YT, 128, 256, SORTED>(A, values, st);
+    case TOKEN_LARGE: return launch_tiles<YT, 64, 256, SORTED>(A, values, st);
     case TOKEN_MID: return launch_few<MIXAQ_I8, YT, 2, 2, 8, SORTED>(A, values, st);
     case TOKEN_SPLIT: return launch_few<MIXAQ_I8, YT, 4, 4, 4, SORTED>(A, values, st);
     case TOKEN_FEW: break;

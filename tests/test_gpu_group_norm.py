@@ -16,7 +16,9 @@ def run(x, y, images, groups, gamma=None, beta=None, act="none", eps=1e-5, y_sca
     return M.mixaq_group_norm(norm, x, y, y_scales, M.alloc_group_norm_workspace(norm, x.shape[0]))
 
 
-SIZES = [(1, 1, 1, 1), (1, 1, 8, 8), (2, 3, 5, 5), (1, 50, 7, 1), (3, 49, 96, 32), (2, 100, 10, 5), (1, 1050, 256, 32), (2, 333, 129, 3), (4, 17, 264, 11), (1, 5000, 24, 3),
+# images, rows, channels, groups: small maps that one kernel takes (of 8 channels and of 24; at, and one row behind, the most that a workgroup holds), widths that are no
+# multiple of 8, groups of a part of 8, of 8 and of more, one channel a group, the most groups and channels
+SIZES = [(2, 4096, 32, 4), (1, 4097, 32, 4), (2, 1364, 48, 16), (1, 1365, 48, 16), (3, 16, 2048, 1), (1, 17, 2048, 1), (1, 1, 1, 1), (1, 1, 8, 8), (2, 3, 5, 5), (1, 50, 7, 1), (3, 49, 96, 32), (2, 100, 10, 5), (1, 1050, 256, 32), (2, 333, 129, 3), (4, 17, 264, 11), (1, 5000, 24, 3),
          (2, 700, 1000, 8), (1, 300, 2048, 32), (5, 9, 1024, 1024), (2, 40, 4095, 35), (1, 30, 8192, 64), (3, 5, 8191, 1), (700, 4, 32, 4), (1, 20000, 96, 32), (8, 2500, 128, 32)]
 
 
