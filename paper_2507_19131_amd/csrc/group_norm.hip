@@ -8,7 +8,7 @@ using namespace mixaq;
 
 namespace {
 
-constexpr int MOST_GROUPS = 1024, MOST_CHANNELS = 8192, THREADS = 1024;
+constexpr int MOST_GROUPS = 1024, MOST_CHANNELS = 8192;
 
 // Sums over values less a pivot, the first value of their image and group: squares of differences from one of the values are at most as many times the
 // variance as there are values, so that binary64 keeps the variance whatever the mean is.
@@ -23,6 +23,8 @@ struct GroupArgs {
     int rows, chunks, chunk_rows;     // of an image
     int units, lanes, act, y_type;    // units: of eight channels; lanes: of a row, of the kernel that writes
     float eps;
+    double inv_count;                 // of a group's values
+    FastDiv by_group;                 // per_group
     const float *gamma, *beta;
     Sums* part;                       // [images][chunks][groups]
     float* pivots;                    // [images][groups]: x may be written over
@@ -38,6 +40,7 @@ __device__ __forceinline__ double shfl64(double v, int from)
 // Which rows and channels a thread takes: of up to 64 units a wave takes whole rows, 64 / units of them, of more the workgroup does.  slot < slots for threads that
 // take any; `left`: how many rows of sums there are once a wave has added up its own.
 struct Place { int u, slot, slots, of_wave, left; };
+template <int THREADS>
 __device__ __forceinline__ Place place_of(int units)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -60,7 +63,7 @@ __device__ __forceinline__ Place place_of(int units)
 
 // Adds up what the threads of a workgroup have for each group, of a unit's eight channels together (WHOLE) or each for itself: the rows of a wave by halves, then 16 lanes a
 // group the rows that are left.  One thread a group calls to(g, sums).  The order goes by the sizes alone.
-template <bool TINY, bool WHOLE, int E, typename To>
+template <int THREADS, bool TINY, bool WHOLE, int E, typename To>
 __device__ __forceinline__ void add_up(double (&v)[E], double (&q)[E], const Place& p, int units, int per_group, int groups, int C, Sums (*red)[THREADS], To to)
 {
     const int lane = threadIdx.x & 63;
@@ -118,24 +121,35 @@ __device__ __forceinline__ void add(double (&v)[E], double (&q)[E], const float 
 
 // What becomes of a group's values: (x - hi) a + b, a = r gamma, b = beta - lo a; hi + lo is the mean.
 struct Factors { float hi, lo, r; };
-__device__ __forceinline__ Factors factors_of(Sums s, double count, float pivot, float eps)
+__device__ __forceinline__ Factors factors_of(Sums s, double n, float pivot, float eps)
 {
-    const double n = 1.0 / count, off = s.v * n, mean = (double)pivot + off, variance = s.q * n - off * off;
+    const double off = s.v * n, mean = (double)pivot + off, variance = s.q * n - off * off;
     Factors f;
     f.hi = (float)mean;
     f.lo = (float)(mean - (double)f.hi);
     f.r = (float)(1.0 / sqrt((variance < 0.0 ? 0.0 : variance) + (double)eps));          // (a NaN stays one)
     return f;
 }
+template <bool TINY>
+__device__ __forceinline__ void load_vectors(const GroupArgs& A, Eight c, float (&gamma)[8], float (&beta)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        gamma[e] = 1.0f;
+        beta[e] = 0.0f;
+    }
+    if (A.gamma) load8f<TINY>(A.gamma, c, A.C, gamma);
+    if (A.beta) load8f<TINY>(A.beta, c, A.C, beta);
+}
+// a: gamma, b: beta
 __device__ __forceinline__ void coefficients(const GroupArgs& A, Eight c, const Factors* of, int first, float (&hi)[8], float (&a)[8], float (&b)[8])
 {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int channel = min(c.at + e, A.C - 1);
-        const Factors f = of[channel / A.per_group - first];
+        const Factors f = of[A.by_group(min(c.at + e, A.C - 1)) - first];
         hi[e] = f.hi;
-        a[e] = f.r * (A.gamma ? A.gamma[channel] : 1.0f);
-        b[e] = fmaf(-f.lo, a[e], A.beta ? A.beta[channel] : 0.0f);
+        a[e] *= f.r;
+        b[e] = fmaf(-f.lo, a[e], b[e]);
     }
 }
 template <typename T>
@@ -155,23 +169,25 @@ __device__ __forceinline__ void store_values(const GroupArgs& A, long long row, 
 
 // Small maps in one kernel: a workgroup holds its channels of an image, whole groups and whole units, in registers.
 constexpr int HELD = 4;                           // rows of a thread
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int parts)
 {
     constexpr int E = WHOLE ? 1 : 8;
     __shared__ Sums red[E][THREADS];
     __shared__ Factors factor[8];                                            // (of lcm(8, per_group) channels)
     const int image = blockIdx.x / parts, part = blockIdx.x - image * parts, width = A.C / parts, units = width / 8;
-    const Place p = place_of(units);
+    const Place p = place_of<THREADS>(units);
     const int slots = p.slots, slot = p.slot, first = part * width / A.per_group;
     const Eight c = {part * width + p.u * 8, 0};
     const T* const map = (const T*)A.x + (long long)image * A.rows * A.ldx;
     T x[HELD][8];
 #pragma unroll
     for (int k = 0; k < HELD; ++k) load8<false>(map + (long long)min(slot + k * slots, A.rows - 1) * A.ldx, c, A.C, x[k]);
+    float hi[8], a[8], b[8];
+    load_vectors<false>(A, c, a, b);
     double pivot[E], v[E] = {}, q[E] = {};
 #pragma unroll
-    for (int e = 0; e < E; ++e) pivot[e] = (double)(float)map[(c.at + e) / A.per_group * A.per_group];
+    for (int e = 0; e < E; ++e) pivot[e] = (double)(float)map[A.by_group(c.at + e) * A.per_group];
     const float mine = (float)map[(first + min((int)threadIdx.x, width / A.per_group - 1)) * A.per_group];         // the pivot of group threadIdx.x
     __shared__ float pivots[8];
     if (threadIdx.x < 8) pivots[threadIdx.x] = mine;
@@ -183,11 +199,10 @@ __global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int p
             for (int e = 0; e < 8; ++e) f[e] = (float)x[k][e];
             add<WHOLE>(v, q, f, pivot);
         }
-    add_up<false, WHOLE>(v, q, p, units, A.per_group, width / A.per_group, width, red, [&](int g, Sums s) {
-        factor[g] = factors_of(s, (double)A.rows * A.per_group, pivots[g], A.eps);
+    add_up<THREADS, false, WHOLE>(v, q, p, units, A.per_group, width / A.per_group, width, red, [&](int g, Sums s) {
+        factor[g] = factors_of(s, A.inv_count, pivots[g], A.eps);
     });
     __syncthreads();                                                         // (every value has been read: y may be x)
-    float hi[8], a[8], b[8];
     coefficients(A, c, factor, first, hi, a, b);
     if (slot >= slots) return;
 #pragma unroll
@@ -199,32 +214,32 @@ __global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int p
     }
 }
 
-constexpr int AHEAD = 4;                          // rows of a thread that are on their way at one time
+constexpr int AHEAD = 8;                          // rows of a thread that are on their way at one time (of 32 bits half as many)
 
 // The sums of one chunk of rows.  A thread keeps to eight channels, so that the threads of a workgroup read whole rows one behind the other.  WHOLE: a
 // group is a multiple of eight channels, whose sums a thread takes together.
-template <typename T, bool TINY, bool WHOLE>
+template <typename T, bool TINY, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_sums_kernel(GroupArgs A)
 {
-    constexpr int E = WHOLE ? 1 : 8;
+    constexpr int E = WHOLE ? 1 : 8, TURN = AHEAD / (sizeof(T) == 4 ? 2 : 1) / (THREADS == 1024 ? 2 : 1);
     __shared__ Sums red[E][THREADS];
     const int image = blockIdx.x / A.chunks, chunk = blockIdx.x - image * A.chunks;
-    const Place p = place_of(A.units);
+    const Place p = place_of<THREADS>(A.units);
     const int slots = p.slots, slot = p.slot;
     const Eight c = place8<TINY>(p.u * 8, A.C);
     const T* const map = (const T*)A.x + (long long)image * A.rows * A.ldx;
     double pivot[E], v[E] = {}, q[E] = {};
 #pragma unroll
-    for (int e = 0; e < E; ++e) pivot[e] = (double)(float)map[min(c.at + e, A.C - 1) / A.per_group * A.per_group];
+    for (int e = 0; e < E; ++e) pivot[e] = (double)(float)map[A.by_group(min(c.at + e, A.C - 1)) * A.per_group];
     if (slot < slots) {
         const int end = min((chunk + 1) * A.chunk_rows, A.rows);
         int r = chunk * A.chunk_rows + slot;
-        for (; r + (AHEAD - 1) * slots < end; r += AHEAD * slots) {
-            T x[AHEAD][8];
+        for (; r + (TURN - 1) * slots < end; r += TURN * slots) {
+            T x[TURN][8];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) load8<TINY>(map + (long long)(r + k * slots) * A.ldx, c, A.C, x[k]);
+            for (int k = 0; k < TURN; ++k) load8<TINY>(map + (long long)(r + k * slots) * A.ldx, c, A.C, x[k]);
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
+            for (int k = 0; k < TURN; ++k) {
                 float f[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = (float)x[k][e];
@@ -237,7 +252,7 @@ __global__ __launch_bounds__(THREADS) void group_sums_kernel(GroupArgs A)
             add<WHOLE>(v, q, f, pivot);
         }
     }
-    add_up<TINY, WHOLE>(v, q, p, A.units, A.per_group, A.groups, A.C, red, [&](int g, Sums s) {
+    add_up<THREADS, TINY, WHOLE>(v, q, p, A.units, A.per_group, A.groups, A.C, red, [&](int g, Sums s) {
         A.part[((long long)image * A.chunks + chunk) * A.groups + g] = s;
         if (chunk == 0) A.pivots[(long long)image * A.groups + g] = (float)map[g * A.per_group];
     });
@@ -246,10 +261,10 @@ __global__ __launch_bounds__(THREADS) void group_sums_kernel(GroupArgs A)
 // Chunk by chunk again, from its last rows, which the caches are likely to hold, to the first: every workgroup adds up its image's sums first, in an order that goes
 // by the sizes alone, while its first rows are on their way.  `lanes` lanes a row: for values as many as it has units of eight channels, for codes a power of
 // two, whose maximum goes through the lanes and, of more than a wave, through LDS.
-template <typename T, bool TINY>
+template <typename T, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
 {
-    constexpr int TURN = sizeof(T) == 4 ? AHEAD / 2 : AHEAD;
+    constexpr int TURN = AHEAD / (sizeof(T) == 4 ? 2 : 1) / (THREADS == 1024 ? 2 : 1);
     __shared__ Sums merge[THREADS];
     __shared__ Factors factor[MOST_GROUPS];
     __shared__ unsigned part[2][THREADS / 64];
@@ -266,30 +281,40 @@ __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
     };
     int r0 = first + (end - 1 - first) / step * step;
     request(r0);
+    float hi[8], a[8], b[8];
+    load_vectors<TINY>(A, c, a, b);
     {
-        const int teams = THREADS / A.groups, g = threadIdx.x % A.groups, l = threadIdx.x / A.groups;
+        const int at_once = min(A.groups, THREADS), teams = THREADS / at_once, l = threadIdx.x / at_once;
         int fold = 1;                                                        // the largest power of two up to teams and chunks
         while (fold * 2 <= teams && fold * 2 <= A.chunks) fold *= 2;
-        if (l < fold) {
+        for (int g = threadIdx.x - l * at_once; g < A.groups; g += at_once) {            // (once, unless a thread has a group or two)
             Sums s = {0.0, 0.0};
-            for (int i = l; i < A.chunks; i += fold) {
-                const Sums o = A.part[((long long)image * A.chunks + i) * A.groups + g];
-                s.v += o.v;
-                s.q += o.q;
+            if (l < fold) {
+                const Sums* const from = A.part + (long long)image * A.chunks * A.groups + g;
+                for (int i = l; i < A.chunks; i += 8 * fold) {               // (each from beyond the L2: eight on their way at one time)
+                    Sums o[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] = from[(long long)min(i + k * fold, A.chunks - 1) * A.groups];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const bool one = i + k * fold < A.chunks;
+                        s.v += one ? o[k].v : 0.0;
+                        s.q += one ? o[k].q : 0.0;
+                    }
+                }
+                merge[threadIdx.x] = s;
             }
-            merge[threadIdx.x] = s;
-        }
-        for (int d = fold / 2; d; d /= 2) {
-            __syncthreads();
-            if (l < d) {
-                merge[threadIdx.x].v += merge[threadIdx.x + d * A.groups].v;
-                merge[threadIdx.x].q += merge[threadIdx.x + d * A.groups].q;
+            for (int d = fold / 2; d; d /= 2) {
+                __syncthreads();
+                if (l < d) {
+                    merge[threadIdx.x].v += merge[threadIdx.x + d * at_once].v;
+                    merge[threadIdx.x].q += merge[threadIdx.x + d * at_once].q;
+                }
             }
+            if (l == 0) factor[g] = factors_of(merge[threadIdx.x], A.inv_count, A.pivots[(long long)image * A.groups + g], A.eps);
         }
-        if (l == 0) factor[g] = factors_of(merge[g], (double)A.rows * A.per_group, A.pivots[(long long)image * A.groups + g], A.eps);
     }
     __syncthreads();
-    float hi[8], a[8], b[8];
     coefficients(A, c, factor, 0, hi, a, b);
     int turn = 0;
     for (;;) {
@@ -325,11 +350,13 @@ __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
 }
 
 // Chunks of an image: a workgroup a CU in all (what every one adds up first grows with their number), each with rows for a turn of AHEAD or more.
-int slots_of(int units) { return units <= 64 ? 64 / units * (THREADS / 64) : THREADS / units; }
+constexpr int THREADS = 512, MOST_THREADS_EACH = 1024;                       // of a workgroup, of one for more than 4096 channels
+int threads_of(int units) { return units > THREADS ? MOST_THREADS_EACH : THREADS; }
+int slots_of(int units, int threads) { return units <= 64 ? 64 / units * (threads / 64) : threads / units; }
 struct Chunks { int count, rows; };
 Chunks chunks_of(int rows, int images, int units)
 {
-    const int turn = slots_of(units);
+    const int turn = slots_of(units, threads_of(units));
     const long long most = ((long long)rows + AHEAD * turn - 1) / (AHEAD * turn), wanted = std::max(1, (256 + images - 1) / images);
     const int count = (int)std::min(most, wanted), per = (rows + count - 1) / count;
     return {(rows + per - 1) / per, per};
@@ -363,30 +390,31 @@ int parts_of(const mixaq_group_norm_desc& d)
 {
     int width = d.C / d.groups;
     while (width % 8) width += d.C / d.groups;                               // (after at most eight)
-    if (d.C % 8 || d.C % width || width / 8 > THREADS || (d.rows_per_image - 1LL) / slots_of(width / 8) >= HELD) return 0;
+    if (d.C % 8 || d.C % width || width / 8 > 1024 || (d.rows_per_image - 1LL) / slots_of(width / 8, 1024) >= HELD) return 0;
     return d.C / width;
 }
 
 template <typename T>
 void launch_small(const GroupArgs& A, int parts, unsigned blocks, hipStream_t st)
 {
-    if (A.per_group % 8 == 0) hipLaunchKernelGGL((group_small_kernel<T, true>), dim3(blocks), dim3(THREADS), 0, st, A, parts);
-    else hipLaunchKernelGGL((group_small_kernel<T, false>), dim3(blocks), dim3(THREADS), 0, st, A, parts);
+    if (A.per_group % 8 == 0) hipLaunchKernelGGL((group_small_kernel<T, true, 1024>), dim3(blocks), dim3(1024), 0, st, A, parts);
+    else hipLaunchKernelGGL((group_small_kernel<T, false, 1024>), dim3(blocks), dim3(1024), 0, st, A, parts);
 }
-template <typename T, bool TINY>
+template <typename T, bool TINY, int THREADS>
 void launch(const GroupArgs& A, unsigned blocks, hipStream_t st)
 {
-    if (A.per_group % 8 == 0) hipLaunchKernelGGL((group_sums_kernel<T, TINY, true>), dim3(blocks), dim3(THREADS), 0, st, A);
-    else hipLaunchKernelGGL((group_sums_kernel<T, TINY, false>), dim3(blocks), dim3(THREADS), 0, st, A);
-    hipLaunchKernelGGL((group_norm_kernel<T, TINY>), dim3(blocks), dim3(THREADS), 0, st, A);
+    if (A.per_group % 8 == 0) hipLaunchKernelGGL((group_sums_kernel<T, TINY, true, THREADS>), dim3(blocks), dim3(THREADS), 0, st, A);
+    else hipLaunchKernelGGL((group_sums_kernel<T, TINY, false, THREADS>), dim3(blocks), dim3(THREADS), 0, st, A);
+    hipLaunchKernelGGL((group_norm_kernel<T, TINY, THREADS>), dim3(blocks), dim3(THREADS), 0, st, A);
 }
 template <int TYPE>
 void launch_type(const GroupArgs& A, int parts, unsigned blocks, hipStream_t st)
 {
     using T = typename TypeOf<TYPE>::T;
     if (parts) launch_small<T>(A, parts, blocks, st);
-    else if (A.C < 8) launch<T, true>(A, blocks, st);
-    else launch<T, false>(A, blocks, st);
+    else if (A.C < 8) launch<T, true, THREADS>(A, blocks, st);
+    else if (A.units <= THREADS) launch<T, false, THREADS>(A, blocks, st);
+    else launch<T, false, MOST_THREADS_EACH>(A, blocks, st);
 }
 
 }  // namespace
@@ -443,11 +471,13 @@ int mixaq_group_norm(const mixaq_group_norm_desc* desc, const mixaq_group_norm_p
     A.rows = d.rows_per_image; A.chunks = ch.count; A.chunk_rows = ch.rows;
     A.act = d.activation; A.eps = d.eps;
     A.gamma = params->gamma; A.beta = params->beta;
+    A.inv_count = 1.0 / ((double)d.rows_per_image * A.per_group);
+    A.by_group = FastDiv(A.per_group);
     A.part = (Sums*)workspace;
     A.pivots = (float*)((char*)workspace + sums_bytes(d, images));
     const int parts = y->type == MIXAQ_I8 ? 0 : parts_of(d);
     const long long blocks = (long long)images * (parts ? parts : ch.count);
-    if (blocks * THREADS >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d images are too many for one call", images);
+    if (blocks * 1024 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d images are too many for one call", images);
     if (x->type == MIXAQ_F32) launch_type<MIXAQ_F32>(A, parts, (unsigned)blocks, (hipStream_t)stream);
     else if (x->type == MIXAQ_F16) launch_type<MIXAQ_F16>(A, parts, (unsigned)blocks, (hipStream_t)stream);
     else launch_type<MIXAQ_BF16>(A, parts, (unsigned)blocks, (hipStream_t)stream);
