@@ -83,12 +83,9 @@ __device__ __forceinline__ int source_of(const TokenArgs& A, int r)
 // A workgroup of NW waves computes 16 MR rows times NR tiles of 16 outputs, wave w the blocks w, w + NW, .. of K; the waves' sums meet in LDS.
 // x may be given as values: the waves look for the rows' maxima first, each in its blocks, and quantize what they multiply.  SORTED: a workgroup takes
 // all rows of its expert, one tile after the other.
-template <int XT>
-__device__ __forceinline__ void values_of(const void* row, int k0, int K, float (&v)[32])     // 16 from k0 on, 16 from k0 + 64 on
+template <typename T>
+__device__ __forceinline__ void values_of(const T* from, int k0, int K, T (&t)[2][16])        // 16 from k0 on, 16 from k0 + 64 on
 {
-    using T = typename TypeOf<XT>::T;
-    const T* const from = (const T*)row;
-    T t[2][16];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int k = k0 + h * 64;
@@ -97,12 +94,27 @@ __device__ __forceinline__ void values_of(const void* row, int k0, int K, float 
 #pragma unroll
             for (int e = 0; e < 16; ++e) t[h][e] = k + e < K ? from[k + e] : (T)0.0f;
     }
+}
+template <typename T>
+__device__ __forceinline__ unsigned largest_of(const T (&t)[2][16])
+{
+    unsigned m = 0;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] = (float)t[e >> 4][e & 15];
+    for (int e = 0; e < 32; ++e) m = max(m, magnitude((float)t[e >> 4][e & 15]));
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ void operands_of(const T (&t)[2][16], float inv, v4i (&x)[2])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const T* const f = &t[i >> 2][4 * (i & 3)];
+        x[i >> 2][i & 3] = int_codes4((float)f[0], (float)f[1], (float)f[2], (float)f[3], inv);
+    }
 }
 
 template <int XT, int YT, int MR, int NR, int NW, bool SORTED>
-__global__ __launch_bounds__(NW * 64) void token_few_kernel(TokenArgs A, int per, FastDiv by_per, int groups)
+__global__ __launch_bounds__(NW * 64, XT == MIXAQ_I8 && MR == 1 ? 4 : 1) void token_few_kernel(TokenArgs A, int per, FastDiv by_per, int groups)
 {
     constexpr int FR = MR * NR;                                              // 16 x 16 results of the workgroup
     constexpr bool FROM_CODES = XT == MIXAQ_I8;
@@ -112,37 +124,78 @@ __global__ __launch_bounds__(NW * 64) void token_few_kernel(TokenArgs A, int per
     __shared__ float scale_of[16 * MR];
     __shared__ int source[16 * MR];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-    // a run of workgroups per XCD; the row tiles of one run of weights beside one another
-    const int per_xcd = (groups + 7) / 8, t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per_xcd || t >= groups) return;            // the whole workgroup
+    // a run of workgroups per XCD, the row tiles of one run of weights beside one another; of rows sorted by expert every XCD has a share of each expert, of
+    // which some may have no rows
+    const int per_xcd = (groups + 7) / 8, t = SORTED ? (int)blockIdx.x : (int)((blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3));
+    if ((!SORTED && (int)(blockIdx.x >> 3) >= per_xcd) || t >= groups) return;           // the whole workgroup
     const int q = by_per(t), in = t - q * per, nt = SORTED ? in : q, nb = nt * NR / 8, tile0 = nt * NR % 8;
     if (nb * SBLOCK + output_of(tile0, 0) >= A.N) return;                    // (the tiles of the last block may all lie beyond)
     int first = in * 16 * MR, end = A.M;
     if (SORTED) rows_of(A, q, first, end);
     const long long layer = SORTED ? (long long)q * A.NB : 0;                // blocks of 128 outputs before this expert's
     const v4i* const w0 = (const v4i*)(A.w + ((layer + nb) * A.KB * 8 + tile0) * TILE_BYTES) + lane;
+    constexpr int MINE = (FR + NW - 1) / NW;                                 // results that a wave sums and finishes
+    v4f sw[MINE], bias[MINE];
+    if (!SORTED || first < end) {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const long long n0 = (layer + nb) * SBLOCK + output_of(tile0 + min(wave + i * NW, FR - 1) % NR, 4 * g);
+            __builtin_memcpy(&sw[i], A.sw + n0, 16);
+            __builtin_memcpy(&bias[i], A.bias + n0, 16);
+        }
+    }
+    struct Operands { v4i w[NR][2], x[MR][2]; };
     for (int r0 = first; r0 < (SORTED ? end : first + 1); r0 += 16 * MR) {
         const X* from[MR];
         int src[MR];
+        RowScale s[MR];
+        auto load_w = [&](int kb, Operands& o) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                o.w[n][0] = w0[(kb * 8 + n) * 128];
+                o.w[n][1] = w0[(kb * 8 + n) * 128 + 64];
+            }
+        };
+        auto load_x = [&](int kb, Operands& o) {                             // (behind a row's end the row's first codes: the weights there are zero)
+            const int k0 = kb * SBLOCK + g * 16;
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+                if constexpr (FROM_CODES) {
+                    o.x[m][0] = *(const v4i*)(from[m] + (k0 < A.K ? k0 : 0));
+                    o.x[m][1] = *(const v4i*)(from[m] + (k0 + 64 < A.K ? k0 + 64 : 0));
+                } else {
+                    X t[2][16];
+                    values_of(from[m], k0, A.K, t);
+                    operands_of(t, s[m].inv, o.x[m]);
+                }
+            }
+        };
+        Operands now;
+        const bool works = wave < A.KB;
+        if (works) load_w(wave, now);                                        // on their way while the rows are looked up
 #pragma unroll
         for (int m = 0; m < MR; ++m) {
             const int r = min(r0 + m * 16 + c, end - 1);
             src[m] = SORTED ? source_of(A, r) : r;
             from[m] = (const X*)A.x + (long long)max(src[m], 0) * A.ldx;
         }
-        RowScale s[MR];
         if constexpr (FROM_CODES) {
 #pragma unroll
             for (int m = 0; m < MR; ++m) s[m].scale = A.sx[max(src[m], 0)];
+            if (works) load_x(wave, now);
         } else {
+            X t[MR][2][16];                                                  // the first block stays in registers until its row's scale is known
 #pragma unroll
             for (int m = 0; m < MR; ++m) {
                 unsigned largest = 0;
-                for (int kb = wave; kb < A.KB; kb += NW) {
-                    float v[32];
-                    values_of<XT>(from[m], kb * SBLOCK + g * 16, A.K, v);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) largest = max(largest, magnitude(v[e]));
+                if (works) {
+                    values_of(from[m], wave * SBLOCK + g * 16, A.K, t[m]);
+                    largest = largest_of(t[m]);
+                }
+                for (int kb = wave + NW; kb < A.KB; kb += NW) {
+                    X u[2][16];
+                    values_of(from[m], kb * SBLOCK + g * 16, A.K, u);
+                    largest = max(largest, largest_of(u));
                 }
                 largest = over4rows(largest, MaxOf());
                 if (g == 0) top[wave][m * 16 + c] = largest;
@@ -154,36 +207,28 @@ __global__ __launch_bounds__(NW * 64) void token_few_kernel(TokenArgs A, int per
 #pragma unroll
                 for (int w = 0; w < NW; ++w) largest = max(largest, top[w][m * 16 + c]);
                 s[m] = row_scale(largest);
+                if (works) operands_of(t[m], s[m].inv, now.x[m]);
             }
         }
         v4i acc[MR][NR] = {};
-        for (int kb = wave; kb < A.KB; kb += NW) {
-            v4i w[NR][2], x[MR][2];
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                w[n][0] = w0[(kb * 8 + n) * 128];
-                w[n][1] = w0[(kb * 8 + n) * 128 + 64];
-            }
-            const int k0 = kb * SBLOCK + g * 16;
-#pragma unroll
-            for (int m = 0; m < MR; ++m) {
-                if constexpr (FROM_CODES) {
-                    x[m][0] = *(const v4i*)(from[m] + (k0 < A.K ? k0 : 0));
-                    x[m][1] = *(const v4i*)(from[m] + (k0 + 64 < A.K ? k0 + 64 : 0));
-                } else {
-                    float v[32];
-                    values_of<XT>(from[m], k0, A.K, v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[m][i >> 2][i & 3] = int_codes4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], s[m].inv);
-                }
-            }
+        auto multiply = [&](const Operands& o) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int m = 0; m < MR; ++m) {
-                    acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[n][0], x[m][0], acc[m][n], 0, 0, 0);
-                    acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[n][1], x[m][1], acc[m][n], 0, 0, 0);
+                    acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.w[n][0], o.x[m][0], acc[m][n], 0, 0, 0);
+                    acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.w[n][1], o.x[m][1], acc[m][n], 0, 0, 0);
                 }
+        };
+        if (works) {                                                         // one block's operands travel under the products of the last one
+            for (int kb = wave + NW; kb < A.KB; kb += NW) {
+                Operands next;
+                load_w(kb, next);
+                load_x(kb, next);
+                multiply(now);
+                now = next;
+            }
+            multiply(now);
         }
 #pragma unroll
         for (int m = 0; m < MR; ++m) {
@@ -198,19 +243,16 @@ __global__ __launch_bounds__(NW * 64) void token_few_kernel(TokenArgs A, int per
         using T = typename TypeOf<YT>::T;
         const int used = min(NW, A.KB);
 #pragma unroll
-        for (int i = 0; i < (FR + NW - 1) / NW; ++i) {                       // results that a wave sums and finishes
+        for (int i = 0; i < MINE; ++i) {
             const int f = wave + i * NW;
             if (f >= FR) break;
             v4i sum = part[0][f][lane];
             for (int w = 1; w < used; ++w) sum += part[w][f][lane];
             const int own = f / NR * 16 + c, r = r0 + own, n0 = nb * SBLOCK + output_of(tile0 + f % NR, 4 * g);
             const float sx = scale_of[own];
-            v4f sw, b;
-            __builtin_memcpy(&sw, A.sw + layer * SBLOCK + n0, 16);
-            __builtin_memcpy(&b, A.bias + layer * SBLOCK + n0, 16);
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fmaf((float)sum[e], sx * sw[e], b[e]);
+            for (int e = 0; e < 4; ++e) v[e] = fmaf((float)sum[e], sx * sw[i][e], bias[i][e]);
             activate(v, A.act);
             if (source[own] < 0) continue;
             T out[4];
@@ -515,7 +557,7 @@ __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kern
 // Four waves side by side, all 32 MT rows and 64 outputs each.  Packed weights lie as the instruction takes them, so a wave loads its own into registers, four
 // steps ahead, and no weight comes twice; x goes through two LDS buffers of 128.
 template <int YT, int MT, bool SORTED>
-__global__ __launch_bounds__(256, MT == 2 ? 4 : 2) void token_wide_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
+__global__ __launch_bounds__(256, 2) void token_wide_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
 {
     constexpr int TM = 32 * MT, XP = TM / 8, XL = XP / 4;                    // 1 KB pieces of a stage, a wave's
     __shared__ v4i xs[2][XP * 64];
@@ -578,7 +620,7 @@ __global__ __launch_bounds__(256, MT == 2 ? 4 : 2) void token_wide_kernel(TokenA
                 __builtin_amdgcn_sched_barrier(0);
                 if (m == MT - 1) load(kb + 1, c, T);
                 if (p < MT) read(c == 3 ? kb + 1 : kb, (c + 1) & 3, p);
-                if (c == 3 && p % 2 == 1 && p < XL + (XL == 2)) request(kb + 2, p - 1);
+                if (c == 3 && p % 2 == 1 && p < XL) request(kb + 2, p - 1);
             }
         }
     }
@@ -631,21 +673,24 @@ int launch_linear(const TokenArgs& A, TokenForm form, int x_type, const mixaq_ro
     switch (form) {
     case TOKEN_TILE: return launch_tiles<YT, 128, 128, SORTED>(A, values, st);
     case TOKEN_WIDE: return launch_tiles<YT, 128, 256, SORTED>(A, values, st);
-    case TOKEN_LARGE: return launch_tiles<YT, 64, 256, SORTED>(A, values, st);
     case TOKEN_MID: return launch_few<MIXAQ_I8, YT, 2, 2, 8, SORTED>(A, values, st);
     case TOKEN_SPLIT: return launch_few<MIXAQ_I8, YT, 4, 4, 4, SORTED>(A, values, st);
     case TOKEN_FEW: break;
     }
-    if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT, 1, 1, 8, SORTED>(A, values, st);
-    if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT, 1, 1, 8, SORTED>(A, values, st);
-    if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT, 1, 1, 8, SORTED>(A, values, st);
+    if constexpr (!SORTED) {
+        if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT, 1, 1, 8, SORTED>(A, nullptr, st);
+        if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT, 1, 1, 8, SORTED>(A, nullptr, st);
+        if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT, 1, 1, 8, SORTED>(A, nullptr, st);
+    }
+    // 16 outputs a workgroup, or 64 where those would be more than run at one time
+    if ((SORTED ? A.experts : (A.M + 15LL) / 16) * A.NB * 8 > 1024) return launch_few<MIXAQ_I8, YT, 1, 4, 8, SORTED>(A, values, st);
     return launch_few<MIXAQ_I8, YT, 1, 1, 8, SORTED>(A, values, st);
 }
 
-// the workspace: codes and scales of x, where it is given as values and not quantized on its way into the product
+// the workspace: codes and scales of x, where it is given as values
 size_t workspace_of(const mixaq_token_linear* h, int32_t x_rows, int32_t x_type)
 {
-    if (x_type == MIXAQ_I8 || x_rows == 0 || token_quantized_inside(x_rows, h->KB)) return 0;
+    if (x_type == MIXAQ_I8 || x_rows == 0) return 0;
     return align256((size_t)x_rows * round_up16(h->d.K)) + align256((size_t)x_rows * 4);
 }
 
@@ -716,7 +761,7 @@ int forward(const mixaq_token_linear* h, const mixaq_rows* x, int32_t x_rows, co
     HIP_TRY(hipGetDevice(&device));
     if (device != h->device) return fail(MIXAQ_E_SHAPE, "the layer was created on device %d, device %d is current", h->device, device);
     mixaq_rows codes = *x;
-    const size_t need = workspace_of(h, x_rows, x->type);
+    const size_t need = !sorted && token_quantized_inside(x_rows, h->KB, h->NB) ? 0 : workspace_of(h, x_rows, x->type);
     if (need) {
         if (!workspace) return fail(MIXAQ_E_NULL, "workspace is NULL (%zu bytes needed)", need);
         if (workspace_bytes < need) return fail(MIXAQ_E_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
