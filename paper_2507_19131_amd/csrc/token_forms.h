@@ -12,14 +12,33 @@ enum TokenForm { TOKEN_FEW, TOKEN_MID, TOKEN_SPLIT, TOKEN_TILE, TOKEN_WIDE };
 //     7.3 / 6.4    1 x 4096 x 4096 7.4 / 5.9, 7.2 / 6.0    16 x 4096 x 1024 10.0 / 7.3, 16.0 / 7.3
 inline bool token_quantized_inside(int M, int KB, int NB) { return KB <= 8 && (M + 15LL) / 16 * NB * 8 <= 256; }
 
-// M rows, KB and NB blocks of 128 inputs and outputs; reach: bytes from the first row of codes that a tile may read to behind the last; values: x is quantized inside
-inline TokenForm token_form(int M, int KB, int NB, int experts, bool sorted, long long reach, bool values)
+// M rows, KB and NB blocks of 128 inputs and outputs; reach: bytes from the first row of codes that a tile may read to behind the last.  us of graph replays, to bf16:
+//   FEW, 16 rows by eight waves, 16 outputs, or 64 where those would be over 1024 workgroups.  MID, 32 x 32 by eight waves, where FEW would be over 512 workgroups and
+//     MID is no more than 256, of few blocks of K 512 (few / mid): 64 x 1024 x 1024 3.4 / 4.0    32 x 4096 x 4096 7.5 / 7.6    128 x 1024 x 1024 (512) 4.1 / 4.1 |
+//     256 x 1024 x 1024 5.6 / 4.2    256 x 4096 x 1024 12.5 / 7.6    512 x 1536 x 384 5.9 / 4.8    256 x 512 x 2048 (MID 512) 4.6 / 4.3 |  512 x 1024 x 1024 (512)
+//     5.4 / 5.6    128 x 4096 x 4096 (512) 11.6 / 12.6    1024 x 1536 x 384 (384) 7.1 / 7.7
+//   SPLIT, 64 x 64 by four waves, from 192 tiles (few / split): 1024 x 1536 x 384 (96) 7.1 / 8.6    512 x 4096 x 1024 (128) 12.4 / 14.1 |  2048 x 1536 x 384 (192) 10.3 / 9.2
+//     1024 x 1024 x 1024 (256) 9.0 / 7.1    4096 x 256 x 256 (256) 5.9 / 5.2    1024 x 4096 x 1024 (256) 22.2 / 14.7
+//   TILE, 128 x 128, from 96 tiles (split / tile): 1024 x 4096 x 1024 (64) 14.7 / 21.3    4096 x 256 x 256 (64) 5.2 / 5.8 |  1024 x 384 x 1536 (96) 6.8 / 6.7
+//     4096 x 1536 x 384 (96) 13.6 / 11.1    512 x 4096 x 4096 (128) 24.3 / 21.8    8192 x 256 x 256 (128) 6.3 / 6.3
+//   WIDE, 128 x 256, from 256 tiles and two blocks of K, of more than one block of outputs (tile / wide): 4096 x 384 x 1536 (192) 9.3 / 10.2    68208 x 96 x 384 (one block
+//     of K) 21.7 / 23.8    68208 x 384 x 96 17.1 / 22.9 |  4096 x 512 x 2048 (256) 11.3 / 11.7    8192 x 1024 x 1024 (256) 16.8 / 16.1    17000 x 192 x 768 (399) 15.1 / 14.1
+//     8192 x 4096 x 1024 (256) 43 / 36    16384 x 4096 x 4096 325 / 255
+// Rows sorted by expert (the average expert stands for all): FEW up to 16 rows an expert, where a workgroup takes all rows of its expert, else tiles (few / tile / wide,
+// 1024 x 2048, 32 experts): 16 rows in all 5.6 / 10.3 / 13.1    256 14.4 / 16.9 / 18.2    512 16.7 / 17.2 / 18.3 |  1024 26.1 / 18.5 / 18.8    4096 74 / 28.5 / 25.7
+inline TokenForm token_form(int M, int KB, int NB, int experts, bool sorted, long long reach)
 {
-    if (values) return TOKEN_FEW;
-    const long long rows = sorted ? std::max(1, M / experts) : M, each = (rows + 127) / 128 * NB, tiles128 = sorted ? each * experts : each;
-    if (rows <= 32 || tiles128 < 64) return TOKEN_FEW;
+    const long long rows = sorted ? M / experts : M, many = sorted ? experts : 1;
+    if (rows <= 16) return TOKEN_FEW;
+    auto tiles = [&](int side) { return (rows + side - 1) / side * many * NB * (128 / side); };
+    if (!sorted) {
+        if (tiles(16) <= 512) return TOKEN_FEW;
+        if (tiles(32) <= (KB <= 4 ? 512 : 256)) return TOKEN_MID;
+        if (tiles(64) < 192) return TOKEN_FEW;
+        if (tiles(128) < 96) return TOKEN_SPLIT;
+    }
     if (reach >= 1LL << 32) return TOKEN_SPLIT;                              // (the tiles count in 32 bits)
-    return tiles128 < 1024 ? TOKEN_TILE : TOKEN_WIDE;
+    return NB > 1 && KB > 1 && (rows + 127) / 128 * many * ((NB + 1) / 2) >= 256 ? TOKEN_WIDE : TOKEN_TILE;
 }
 
 }  // namespace mixaq

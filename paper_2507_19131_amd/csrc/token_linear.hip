@@ -673,7 +673,8 @@ int launch_linear(const TokenArgs& A, TokenForm form, int x_type, const mixaq_ro
     switch (form) {
     case TOKEN_TILE: return launch_tiles<YT, 128, 128, SORTED>(A, values, st);
     case TOKEN_WIDE: return launch_tiles<YT, 128, 256, SORTED>(A, values, st);
-    case TOKEN_MID: return launch_few<MIXAQ_I8, YT, 2, 2, 8, SORTED>(A, values, st);
+    case TOKEN_MID:
+        if constexpr (!SORTED) return launch_few<MIXAQ_I8, YT, 2, 2, 8, SORTED>(A, values, st);
     case TOKEN_SPLIT: return launch_few<MIXAQ_I8, YT, 4, 4, 4, SORTED>(A, values, st);
     case TOKEN_FEW: break;
     }
@@ -780,7 +781,7 @@ int forward(const mixaq_token_linear* h, const mixaq_rows* x, int32_t x_rows, co
     A.M = rows; A.x_rows = x_rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
     A.act = h->d.activation; A.experts = h->d.experts;
     const mixaq_rows* const values = need ? x : nullptr;
-    const TokenForm form = token_form(rows, A.KB, A.NB, h->d.experts, sorted != nullptr, (sorted ? x_rows : 256LL) * A.ldx, codes.type != MIXAQ_I8);
+    const TokenForm form = codes.type != MIXAQ_I8 ? TOKEN_FEW : token_form(rows, A.KB, A.NB, h->d.experts, sorted != nullptr, (sorted ? x_rows : 128LL) * A.ldx);
     if (sorted) {
         A.offsets = sorted->offsets; A.gather = sorted->gather; A.weights = sorted->weights;
         if (y->type == MIXAQ_F32) return launch_linear<MIXAQ_F32, true>(A, form, codes.type, values, st);

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import token_forms as S
 import token_ref as R
 
 pytestmark = pytest.mark.gpu
@@ -120,12 +121,8 @@ def test_rows_of_special_values(cols):
 
 
 # ---------------------------------------------------------------- layers
-SIZES = [(1, 1, 1), (1, 1000, 333), (3, 16, 8), (15, 4400, 130), (16, 128, 16), (17, 127, 129), (40, 1024, 512), (130, 1000, 333), (300, 100, 600), (513, 784, 1030), (700, 1500, 200),
-         (1100, 640, 1024), (2100, 384, 1500), (4800, 96, 400), (9000, 790, 1300)]
-
-
 @pytest.mark.parametrize("y_kind", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("rows,K,N", SIZES)
+@pytest.mark.parametrize("rows,K,N", S.SIZES)
 def test_layer_to_the_last_bit(rows, K, N, y_kind):
     """Without an activation every step has one nearest result.  Behind a row's columns x holds a pattern, and y keeps one."""
     with Layer(rows + K, N, K, bias=N % 2 == 0) as layer:
@@ -257,9 +254,7 @@ def check_sorted(layer, codes, scales, counts, first, y, kind, gather=None, weig
 
 
 @pytest.mark.parametrize("act,kind", [("none", "bf16"), ("silu", "f32"), ("gelu", "f16")])
-@pytest.mark.parametrize("experts,rows,K,N,empty", [
-    (1, 1, 64, 40, ()), (1, 700, 200, 300, ()), (4, 3, 300, 200, ()), (8, 16, 1000, 333, (0,)), (33, 64, 128, 130, (3, 32)), (8, 900, 384, 500, (0, 3, 7)), (5, 2500, 257, 130, (4,)),
-    (64, 6000, 130, 270, (10, 11, 12)), (70, 5000, 96, 64, (0, 63, 64, 69)), (300, 2000, 40, 33, (150,)), (3, 9000, 500, 700, ())])
+@pytest.mark.parametrize("experts,rows,K,N,empty", S.SORTED)
 def test_sorted_rows(experts, rows, K, N, empty, act, kind):
     counts, first, spare = counts_of(experts + rows, experts, rows, empty), 3, 130
     total = first + rows + spare
@@ -320,7 +315,8 @@ def test_rows_without_a_scale_stay_among_themselves():
 
 # ---------------------------------------------------------------- calls
 def test_layer_refuses():
-    with Layer(61, 40, 100, experts=2) as two, Layer(62, 40, 100) as one:
+    with Layer(61, 40, 100, experts=2) as two, Layer(62, 40, 100) as one, Layer(62, 5000, 100) as wide:       # (the wide one quantizes values in a launch of its own)
+        z = torch.empty(70, 5000, device="cuda")
         x, s, y = placed(values(63, 70, 100), "bf16"), placed(values(63, 70, 100), "i8"), Room(70, 40, "f32")
         off = offsets_of([30, 40])
         ws = M.alloc_token_linear_workspace(one.h, 70, torch.bfloat16)
@@ -331,9 +327,10 @@ def test_layer_refuses():
             assert e.value.code == code and words in str(e.value)
 
         refused(-2, "sorted by expert", lambda: M.mixaq_token_linear_forward(two.h, s.t, y.t, x_scales=s.scales))
-        refused(-1, "workspace is NULL", lambda: M.mixaq_token_linear_forward(one.h, x.t, y.t))
-        refused(-4, "needed", lambda: M.mixaq_token_linear_forward(one.h, x.t, y.t, workspace=ws[:-1]))
-        refused(-4, "256-byte", lambda: M.mixaq_token_linear_forward(one.h, x.t, y.t, workspace=torch.cat([ws, ws])[16:]))
+        for call in (lambda w: M.mixaq_token_linear_forward_grouped(two.h, x.t, off, y.t, workspace=w), lambda w: M.mixaq_token_linear_forward(wide.h, x.t, z, workspace=w)):
+            refused(-1, "workspace is NULL", lambda: call(None))
+            refused(-4, "needed", lambda: call(ws[:-1]))
+            refused(-4, "256-byte", lambda: call(torch.cat([ws, ws])[16:]))
         refused(-2, "without a list", lambda: two.grouped(s.t[:60], off, y.t, s.scales[:60]))
         codes, vals, out = M._token_rows(s.t, "x", 0, s.scales), M._rows(x.t, "x", 0), lambda at: M.Rows(at, 40, 0, None, 0)
         plain = lambda a, b, w=None, n=0: M._check(M.load().mixaq_token_linear_forward(one.h, a, 70, b, w, n, None))
@@ -347,7 +344,7 @@ def test_layer_refuses():
             refused(-2, "y and %s" % name, lambda: grouped(out(Y), **{where: Y + size - 4}))
             refused(-2, "%s is not aligned" % name, lambda: grouped(out(Y), **{where: off.data_ptr() + 2}))
             refused(-2, "workspace and %s" % name, lambda: grouped(out(Y), **{where: ws.data_ptr() + 256}, x_=vals, w=ws.data_ptr(), n=ws.numel()))
-        refused(-2, "the workspace overlaps", lambda: plain(vals, out(ws.data_ptr() + 256), ws.data_ptr(), ws.numel()))
+        refused(-2, "the workspace overlaps", lambda: grouped(out(ws.data_ptr() + 256), x_=vals, w=ws.data_ptr(), n=ws.numel()))
         refused(-2, "must be values", lambda: plain(vals, codes, ws.data_ptr(), ws.numel()))
         torch.cuda.synchronize()
         assert bool((y.buffer == FILL).all())
