@@ -22,6 +22,7 @@ struct GroupArgs {
     int C, groups, per_group;         // channels of a group
     int rows, chunks, chunk_rows;     // of an image
     int units, lanes, act, y_type;    // units: of eight channels; lanes: of a row, of the kernel that writes
+    bool aligned;                     // rows of y that are values start at multiples of 16 bytes
     float eps;
     double inv_count;                 // of a group's values
     FastDiv by_group;                 // per_group
@@ -159,12 +160,26 @@ __device__ __forceinline__ void apply(const T (&x)[8], const float (&hi)[8], con
     for (int e = 0; e < 8; ++e) v[e] = fmaf((float)x[e] - hi[e], a[e], b[e]);
     activate(v, act);
 }
-template <bool TINY>
+// PAST: past the caches, where rows start at multiples of 16 bytes.
+template <bool TINY, bool PAST, typename Y>
+__device__ __forceinline__ void store_row(Y* row, Eight c, int C, bool aligned, const float (&v)[8])
+{
+    if (PAST && !TINY && aligned && c.first == 0) {
+        Y t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = (Y)v[e];
+        v4i p[sizeof(Y) / 2];
+        __builtin_memcpy(p, t, sizeof(t));
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Y) / 2; ++i) __builtin_nontemporal_store(p[i], (v4i*)(row + c.at) + i);
+    } else store8<TINY>(row, c, C, v);
+}
+template <bool TINY, bool PAST>
 __device__ __forceinline__ void store_values(const GroupArgs& A, long long row, Eight c, const float (&v)[8])
 {
-    if (A.y_type == MIXAQ_F32) store8<TINY>((float*)A.y + row * A.ldy, c, A.C, v);
-    else if (A.y_type == MIXAQ_F16) store8<TINY>((_Float16*)A.y + row * A.ldy, c, A.C, v);
-    else store8<TINY>((__bf16*)A.y + row * A.ldy, c, A.C, v);
+    if (A.y_type == MIXAQ_F32) store_row<TINY, PAST>((float*)A.y + row * A.ldy, c, A.C, A.aligned, v);
+    else if (A.y_type == MIXAQ_F16) store_row<TINY, PAST>((_Float16*)A.y + row * A.ldy, c, A.C, A.aligned, v);
+    else store_row<TINY, PAST>((__bf16*)A.y + row * A.ldy, c, A.C, A.aligned, v);
 }
 
 // Small maps in one kernel: a workgroup holds its channels of an image, whole groups and whole units, in registers.
@@ -210,7 +225,7 @@ __global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int p
         if (slot + k * slots >= A.rows) break;
         float f[8];
         apply(x[k], hi, a, b, A.act, f);
-        store_values<false>(A, (long long)image * A.rows + slot + k * slots, c, f);
+        store_values<false, false>(A, (long long)image * A.rows + slot + k * slots, c, f);
     }
 }
 
@@ -343,7 +358,7 @@ __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
                     store_int_codes8<TINY>((int8_t*)A.y + row * A.ldy, c, A.C, v[k], s.inv);
                     if (u == 0) A.scales[row] = s.scale;
                 }
-            } else if (real) store_values<TINY>(A, row, c, v[k]);
+            } else if (real) store_values<TINY, true>(A, row, c, v[k]);
         }
         if (r0 < first) break;
     }
@@ -470,6 +485,7 @@ int mixaq_group_norm(const mixaq_group_norm_desc* desc, const mixaq_group_norm_p
     const Chunks ch = chunks_of(d.rows_per_image, images, A.units);
     A.rows = d.rows_per_image; A.chunks = ch.count; A.chunk_rows = ch.rows;
     A.act = d.activation; A.eps = d.eps;
+    A.aligned = (uintptr_t)y->data % 16 == 0 && y->stride * size_of(y->type) % 16 == 0;
     A.gamma = params->gamma; A.beta = params->beta;
     A.inv_count = 1.0 / ((double)d.rows_per_image * A.per_group);
     A.by_group = FastDiv(A.per_group);
