@@ -30,6 +30,7 @@ struct TokenArgs {
     const float* weights;
     long long ldx, ldy;
     int M, x_rows, N, K, KB, NB, act, experts;
+    bool aligned;                     // rows of y start at multiples of 16 bytes
 };
 
 // ---- layouts --------------------------------------------------------------------------------------------------------
@@ -322,7 +323,8 @@ __device__ __forceinline__ void store_rows(const TokenArgs& A, const float (&v)[
             const v4i piece = turn[place(r, p)];
             if (!(kept >> r & 1)) continue;
             T* const to = (T*)A.y + (long long)(row0 + r) * A.ldy + n;
-            if (n + 16 / ES <= A.N) __builtin_memcpy(to, &piece, 16);
+            if (A.aligned && n + 16 / ES <= A.N) __builtin_nontemporal_store(piece, (v4i*)to);
+            else if (n + 16 / ES <= A.N) __builtin_memcpy(to, &piece, 16);
             else {
                 T t[16 / ES];
                 __builtin_memcpy(t, &piece, 16);
@@ -335,16 +337,16 @@ __device__ __forceinline__ void store_rows(const TokenArgs& A, const float (&v)[
     }
 }
 
-// Inclusive sums over the lanes of a wave.
+// Inclusive sums over the lanes of a wave, in the vector unit: within rows of 16, then the last lane of a row to the next one's, of the first half to the second.
+template <int CTRL, int ROWS> __device__ __forceinline__ int from_before(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
 __device__ __forceinline__ int scan64(int v)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d, 64);
-        v += lane >= d ? o : 0;
-    }
-    return v;
+    v += from_before<0x111, 0xf>(v);
+    v += from_before<0x112, 0xf>(v);
+    v += from_before<0x114, 0xf>(v);
+    v += from_before<0x118, 0xf>(v);
+    v += from_before<0x142, 0xa>(v);
+    return v + from_before<0x143, 0xc>(v);
 }
 // Row tiles of TM rows, expert after expert: how many there are in all, and of the t-th its expert and its rows.  By every wave for itself.
 template <int TM>
@@ -778,6 +780,7 @@ int forward(const mixaq_token_linear* h, const mixaq_rows* x, int32_t x_rows, co
     A.sx = codes.scales;
     A.w = h->packed; A.sw = h->scales; A.bias = h->bias;
     A.y = y->data; A.ldy = y->stride;
+    A.aligned = (uintptr_t)y->data % 16 == 0 && y->stride * size_of(y->type) % 16 == 0;
     A.M = rows; A.x_rows = x_rows; A.N = N; A.K = K; A.KB = h->KB; A.NB = h->NB;
     A.act = h->d.activation; A.experts = h->d.experts;
     const mixaq_rows* const values = need ? x : nullptr;
