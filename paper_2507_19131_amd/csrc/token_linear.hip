@@ -83,7 +83,10 @@ __device__ __forceinline__ int source_of(const TokenArgs& A, int r)
 // ---- operands straight from memory, K split over the waves --------------------------------------------------------------------
 // A workgroup of NW waves computes 16 MR rows times NR tiles of 16 outputs, wave w the blocks w, w + NW, .. of K; the waves' sums meet in LDS.
 // x may be given as values: the waves look for the rows' maxima first, each in its blocks, and quantize what they multiply.  SORTED: a workgroup takes
-// all rows of its expert, one tile after the other.
+// all rows of its expert, one tile after the other, so that weights come once.  Weights, rows, scales and bias are asked for as soon as their places are known.
+// What bounds it: a launch and round trips to memory (1 x 1024 x 4096 from codes 3.1 us of a graph replay, 4.2 MB of weights would take 0.8; from values 4.0; 16 rows of
+// 32 experts, 2048 x 1024 each, 5.6 us where the 27 MB of the experts they hit take 5.4), with more rows the operands' way through the caches, each workgroup
+// for itself (256 x 1024 x 1024 in 32 x 32 4.2 us, 1024 x 4096 x 1024 in 64 x 64 14.7).
 template <typename T>
 __device__ __forceinline__ void values_of(const T* from, int k0, int K, T (&t)[2][16])        // 16 from k0 on, 16 from k0 + 64 on
 {
@@ -272,8 +275,10 @@ __global__ __launch_bounds__(NW * 64, XT == MIXAQ_I8 && MR == 1 ? 4 : 1) void to
 }
 
 // ---- both operands through LDS ------------------------------------------------------------------------------------------
-// A workgroup of WM x WN waves computes 32 MT WM rows times 128 WN outputs, a wave 32 MT rows times one block of 128 outputs.  K goes in stages of 64 through a
-// ring of four LDS buffers filled by direct loads, three stages ahead of the products.
+// A workgroup of four waves computes 128 rows times 128 outputs, a wave 32 rows times the outputs.  K goes in stages of 64 through a
+// ring of four LDS buffers filled by direct loads, three stages ahead of the products.  For products whose tiles are few or whose stages are: 4704 x 384 x 1536 with a
+// GELU 11.6 us (444 tiles, two a CU, of six stages: the first loads, the GELU, 14 MB of results), 4704 x 1536 x 384 11.7 (111 tiles: a stage takes 0.35 us, a
+// round trip, however little there is to multiply).
 // Rows of x lie in LDS as 4 chunks of 16 bytes whose places are turned by a fourth of the row's number, so that the 16 lanes that are served
 // together (16 rows, one chunk) meet all 64 banks.
 // The direct loads are asm: as a builtin every LDS read behind them waits for all of them.  They do nothing for stages from `end` on, which the asm finds out: a
@@ -450,62 +455,57 @@ __device__ __forceinline__ void wait_stages(int left)
 
 constexpr int DEPTH = 64, RING = 4;               // bytes of K in a stage, stages in LDS
 
-template <int YT, int MT, int WM, int WN, bool SORTED>
-__global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
+template <int YT, bool SORTED>
+__global__ __launch_bounds__(256, 2) void token_tile_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
 {
-    constexpr int W = WM * WN, TM = 32 * MT * WM;
-    constexpr int XP = TM / 16, WP = WN * 8, XL = XP / W, WL = WP / W, R = XL + WL;      // 1 KB pieces of a stage, of x and of w, and a wave's
-    static_assert(XL % 2 == 0 && WL % 2 == 0 && XP % W == 0 && WP % W == 0, "pairs of whole pieces a wave");
-    __shared__ v4i xs[RING][XP * 64], ws[RING][WP * 64];
+    constexpr int TM = 128, PIECES = 8, OWN = 2, R = 2 * OWN;                // 1 KB pieces of a stage, of x and as many of w, and a wave's
+    __shared__ v4i xs[RING][PIECES * 64], ws[RING][PIECES * 64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5;
-    const int wm = wave / WN, wn = wave % WN, KB = A.KB, stages = (A.K + DEPTH - 1) / DEPTH;
-    int tn, first, end, expert;
-    if (!tile_of<TM, SORTED>(A, tiles_m, tiles_n, by, tn, first, end, expert)) return;       // the whole workgroup
-    const int nb0 = tn * WN, nb = nb0 + wn;
+    const int KB = A.KB, stages = (A.K + DEPTH - 1) / DEPTH;
+    int nb, first, end, expert;
+    if (!tile_of<TM, SORTED>(A, tiles_m, tiles_n, by, nb, first, end, expert)) return;       // the whole workgroup
 
-    // what this wave requests: rows (wave XL + i) 16 + lane / 4 of x, whose lanes take the chunk that belongs in their place, and pieces wave WL + i of w
+    // what this wave requests: rows (2 wave + i) 16 + lane / 4 of x, whose lanes take the chunk that belongs in their place, and pieces 2 wave + i of w
     const int chunk = ((lane & 3) ^ (lane >> 4)) * 16, last_chunk = (A.K - 1) & ~15;      // (what stands behind a row's end is the last chunk again, the weights there are zero)
     const uint8_t* const xb = (const uint8_t*)A.x + (SORTED ? 0 : (long long)first * A.ldx);
-    unsigned from[XL], piece[WL];
+    unsigned from[OWN], piece[OWN];
 #pragma unroll
-    for (int i = 0; i < XL; ++i) {
-        const int r = min(first + (wave * XL + i) * 16 + (lane >> 2), end - 1);
+    for (int i = 0; i < OWN; ++i) {
+        const int r = min(first + (wave * OWN + i) * 16 + (lane >> 2), end - 1);
         from[i] = (unsigned)(SORTED ? max(source_of(A, r), 0) : r - first) * (unsigned)A.ldx;
+        piece[i] = i * TILE_BYTES + lane * 16;
     }
-#pragma unroll
-    for (int i = 0; i < WL; ++i) piece[i] = i * TILE_BYTES + lane * 16;
-    const uint8_t* const wb = A.w + ((long long)expert * A.NB + min(nb0 + wave * WL / 8, A.NB - 1)) * KB * (8 * TILE_BYTES) + wave * WL % 8 * TILE_BYTES;
+    const uint8_t* const wb = A.w + ((long long)expert * A.NB + nb) * KB * (8 * TILE_BYTES) + wave * OWN * TILE_BYTES;
     const unsigned lx = lds_address(xs), lw = lds_address(ws);
-    auto request = [&](int ks, int i) {                                      // two pieces
-        if (i < XL) {
-            const unsigned k = min(ks * DEPTH + chunk, last_chunk);
-            request2(xb, from[i] + k, from[i + 1] + k, lx + (ks % RING * XP + wave * XL + i) * 1024, ks, stages);
-        } else {
-            i -= XL;
-            request2(wb + (long long)(ks >> 1) * (8 * TILE_BYTES) + (ks & 1) * 1024, piece[i], piece[i + 1], lw + (ks % RING * WP + wave * WL + i) * 1024, ks, stages);
-        }
+    const unsigned own = wave * OWN * 1024;
+    auto request_x = [&](int ks) {
+        const unsigned k = min(ks * DEPTH + chunk, last_chunk);
+        request2(xb, from[0] + k, from[1] + k, lx + ks % RING * (PIECES * 1024) + own, ks, stages);
+    };
+    auto request_w = [&](int ks) {
+        request2(wb + (long long)(ks >> 1) * (8 * TILE_BYTES) + (ks & 1) * 1024, piece[0], piece[1], lw + ks % RING * (PIECES * 1024) + own, ks, stages);
     };
     auto meet = [] {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
 #pragma unroll
-    for (int ks = 0; ks < RING; ++ks)
-#pragma unroll
-        for (int i = 0; i < R; i += 2) request(ks, i);
-    const int m0 = wm * 32 * MT;
-    v16i acc[MT][4] = {};
-    v4i x[2][MT], w[2][4];
+    for (int ks = 0; ks < RING; ++ks) {
+        request_x(ks);
+        request_w(ks);
+    }
+    const int m0 = wave * 32;
+    v16i acc[1][4] = {};
+    v4i x[2], w[2][4];
     const v4i* const xr[2] = {&xs[0][(m0 + j) * 4 + (h ^ (j >> 2 & 3))], &xs[0][(m0 + j) * 4 + (h ^ 2 ^ (j >> 2 & 3))]};
-    const v4i* const wr = &ws[0][wn * 512 + (j >> 4) * 64 + h * 16 + (j & 15)];
-    auto read = [&](int ks, int c, int i) {                                  // operand i of step c
-        if (i < MT) x[c][i] = xr[c][ks % RING * (XP * 64) + i * 128];
-        else w[c][i - MT] = wr[ks % RING * (WP * 64) + (i - MT) * 128 + c * 32];
-    };
+    const v4i* const wr = &ws[0][(j >> 4) * 64 + h * 16 + (j & 15)];
+    auto read_x = [&](int ks, int c) { x[c] = xr[c][ks % RING * (PIECES * 64)]; };
+    auto read_w = [&](int ks, int c, int T) { w[c][T] = wr[ks % RING * (PIECES * 64) + T * 128 + c * 32]; };
     wait_stages<R, 3>(stages - 1);
     meet();
+    read_x(0, 0);
 #pragma unroll
-    for (int i = 0; i < MT + 4; ++i) read(0, 0, i);
+    for (int T = 0; T < 4; ++T) read_w(0, 0, T);
     // Of each stage two steps of 32.  What a step's products need is read under those of the step before; behind the last read of a stage the waves
     // meet, and its buffer is requested anew.  The last stage reads on like the others, for nobody.
 #pragma unroll 1
@@ -516,38 +516,43 @@ __global__ __launch_bounds__(WM * WN * 64, MT == 1 ? 2 : 1) void token_tile_kern
                 wait_stages<R, 2>(stages - 2 - ks);
                 meet();
             }
-            constexpr int P = 4 * MT, READS = MT == 1 ? 2 : 1;               // after each of the first products
+            const int next = c == 1 ? ks + 1 : ks;
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int T = p / MT, m = p % MT;
+            for (int T = 0; T < 4; ++T) {
                 __builtin_amdgcn_sched_barrier(0);
-                acc[m][T] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c][T], x[c][m], acc[m][T], 0, 0, 0);
+                acc[0][T] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[c][T], x[c], acc[0][T], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int i = p * READS; i < (p + 1) * READS; ++i)
-                    if (i < MT + 4) read(c == 1 ? ks + 1 : ks, c ^ 1, i);
-                if (c == 1) {
-#pragma unroll
-                    for (int i = p * R / P; i < (p + 1) * R / P; ++i)
-                        if (i % 2 == 0) request(ks + RING, i);
+                if (T == 0) {
+                    read_x(next, c ^ 1);
+                    read_w(next, c ^ 1, 0);
+                    if (c == 1) request_x(ks + RING);
+                } else if (T == 1) {
+                    read_w(next, c ^ 1, 1);
+                    read_w(next, c ^ 1, 2);
+                } else if (T == 2) {
+                    read_w(next, c ^ 1, 3);
+                    if (c == 1) request_w(ks + RING);
                 }
             }
         }
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");              // (and the last reads for nobody)
     meet();
-    if (nb >= A.NB) return;
-    static_assert(RING * XP * 64 >= W * 512, "room for a wave's 32 rows of 256 bytes");
-    finish<YT, MT, 2, SORTED>(A, acc, expert, nb * SBLOCK, first + m0, end, &xs[0][0] + wave * 512);
+    static_assert(RING * PIECES * 64 >= 4 * 512, "room for a wave's 32 rows of 256 bytes");
+    finish<YT, 1, 2, SORTED>(A, acc, expert, nb * SBLOCK, first + m0, end, &xs[0][0] + wave * 512);
 }
 
 // ---- weights straight from memory, x through LDS ------------------------------------------------------------------------------
-// Four waves side by side, all 32 MT rows and 64 outputs each.  Packed weights lie as the instruction takes them, so a wave loads its own into registers, four
-// steps ahead, and no weight comes twice; x goes through two LDS buffers of 128.
-template <int YT, int MT, bool SORTED>
+// Four waves side by side, all 128 rows and 64 outputs each.  Packed weights lie as the instruction takes them, so a wave loads its own into registers, four
+// steps ahead, and no weight comes twice; x goes through two LDS buffers of 128.  With both operands in LDS its reads and the direct loads' writes took as long as the
+// products: 16384 x 4096 x 3840 261 us in 256 x 256 by two times two waves, 254 with the weights in registers, 239 so, where a second workgroup on the CU runs beside
+// a tile's start and end (a library product 278; 8192^3 470, 458, 463, library 453).  What bounds it: the matrix instructions are busy in 59 % of the clocks, and
+// the clock is 1.65 to 1.75 GHz under this load; of 32768 rows of 64 experts x 2048 x 1024 (97 us, unsorted 72) a third as well, 1150 tiles in rounds of 512, which end
+// unevenly.
+template <int YT, bool SORTED>
 __global__ __launch_bounds__(256, 2) void token_wide_kernel(TokenArgs A, int tiles_m, int tiles_n, FastDiv by)
 {
-    constexpr int TM = 32 * MT, XP = TM / 8, XL = XP / 4;                    // 1 KB pieces of a stage, a wave's
+    constexpr int MT = 4, TM = 32 * MT, XP = TM / 8, XL = XP / 4;                    // 1 KB pieces of a stage, a wave's
     __shared__ v4i xs[2][XP * 64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, j = lane & 31, h = lane >> 5, KB = A.KB;
     int tn, first, end, expert;
@@ -649,8 +654,8 @@ int launch_tiles(const TokenArgs& A, const mixaq_rows* values, hipStream_t st)
     const int rc = quantize_first(A, values, st);
     if (rc) return rc;
     const FastDiv by(SORTED ? tiles_n : GROUP_M * tiles_n);
-    if constexpr (TN == 256) hipLaunchKernelGGL((token_wide_kernel<YT, TM / 32, SORTED>), dim3((unsigned)blocks), dim3(256), 0, st, A, (int)tiles_m, tiles_n, by);
-    else hipLaunchKernelGGL((token_tile_kernel<YT, TM / 128, 4, 1, SORTED>), dim3((unsigned)blocks), dim3(256), 0, st, A, (int)tiles_m, tiles_n, by);
+    if constexpr (TN == 256) hipLaunchKernelGGL((token_wide_kernel<YT, SORTED>), dim3((unsigned)blocks), dim3(256), 0, st, A, (int)tiles_m, tiles_n, by);
+    else hipLaunchKernelGGL((token_tile_kernel<YT, SORTED>), dim3((unsigned)blocks), dim3(256), 0, st, A, (int)tiles_m, tiles_n, by);
     HIP_TRY(hipGetLastError());
     return MIXAQ_OK;
 }

@@ -55,7 +55,9 @@ __device__ __forceinline__ unsigned row_top(unsigned m, unsigned* part)
     return m;
 }
 
-// A row is V times eight values in each of G lanes, held in registers between its maximum and its codes: one read of the values.
+// A row is V times eight values in each of G lanes, held in registers between its maximum and its codes: one read of the values.  What bounds it is memory: 68208 x
+// 384 of bf16 13.3 us, 5.9 TB/s (inputs in turn that the last-level cache holds in part), 16384 x 4096 36.6, 5.5 TB/s.  (Codes stored past the caches: 13.1 and 34.9,
+// but the layer that reads them then takes longer by far, 1024 inputs a row through two layers 313 us instead of 214.)
 template <typename T, int G, int V, bool TINY>
 __global__ __launch_bounds__(256) void token_quantize_kernel(QuantArgs A)
 {

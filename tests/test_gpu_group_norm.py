@@ -37,6 +37,16 @@ def test_norm(images, rows, C, groups, x_kind, y_kind, act):
     assert y.untouched() and x.untouched()
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("images,rows,C,groups", [(1, 20000, 96, 32), (2, 3000, 128, 1), (1, 6000, 100, 4), (1, 300, 8192, 64)])
+def test_rows_that_start_at_16_bytes(images, rows, C, groups, kind):
+    """Their whole pieces take another way to memory; what lies between the rows keeps its pattern."""
+    x, y = placed(values(C, images * rows, C), kind), Room(images * rows, C, kind, 8, 8 + -C % 8)
+    run(x.t, y.t, images, groups, act="silu")
+    R.check(y.t, *R.group_norm(x.t, images, groups, 1e-5, None, None, "silu"), kind)
+    assert y.untouched()
+
+
 @pytest.mark.parametrize("gamma,beta", [(True, False), (False, True), (False, False)])
 def test_without_vectors(gamma, beta):
     x = values(3, 200, 96)

@@ -122,11 +122,13 @@ def test_rows_of_special_values(cols):
 
 # ---------------------------------------------------------------- layers
 @pytest.mark.parametrize("y_kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lines", [False, True])
 @pytest.mark.parametrize("rows,K,N", S.SIZES)
-def test_layer_to_the_last_bit(rows, K, N, y_kind):
-    """Without an activation every step has one nearest result.  Behind a row's columns x holds a pattern, and y keeps one."""
+def test_layer_to_the_last_bit(rows, K, N, lines, y_kind):
+    """Without an activation every step has one nearest result.  Behind a row's columns x holds a pattern, and y keeps one.  lines: y's rows start at multiples of
+    16 bytes."""
     with Layer(rows + K, N, K, bias=N % 2 == 0) as layer:
-        x, y = placed(values(rows, rows, K), "i8", 16, 16), Room(rows, N, y_kind, 3, 2)
+        x, y = placed(values(rows, rows, K), "i8", 16, 16), Room(rows, N, y_kind, 8, 8 + -N % 8) if lines else Room(rows, N, y_kind, 3, 2)
         layer.forward(x.t, y.t, x.scales)
         want = R.linear_bits(x.t, x.scales, *layer.matrix(), y_kind)
         R.same(y.t, want)
