@@ -202,6 +202,44 @@ def test_scales_at_both_ends_of_their_range():
         R.same(y, R.linear_bits(x.t, x.scales, *layer.matrix(), "f32"))
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,K,N", [(5, 208, 100), (16, 1000, 333), (60, 1024, 700)])
+def test_values_without_a_scale(rows, K, N, kind):
+    """A NaN or an infinity anywhere in a row makes its results NaN, and no other row's."""
+    with Layer(23, N, K, act="relu") as layer:
+        x = placed(values(24, rows, K), kind)
+        x.t[1, K - 1], x.t[rows - 1, 0], x.t[2] = NAN, -float("inf"), 0.0
+        y = torch.empty(rows, N, device="cuda")
+        layer.forward(x.t, y)
+        codes, scales = R.quantize(x.t)
+        R.check(y, *layer.reference(codes, scales), "f32")
+        assert torch.isnan(y).all(1).nonzero().flatten().tolist() == [1, rows - 1] and torch.isnan(y).any(1).sum() == 2
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "silu", "relu"])
+@pytest.mark.parametrize("rows", [16, 40000])
+def test_activations_of_any_value(rows, act):
+    """One input, one output, weight 1: the value is the row's scale, of either sign, from the smallest to infinity."""
+    gen = torch.Generator().manual_seed(rows)
+    v = 10.0 ** (76 * torch.rand(rows, generator=gen, dtype=torch.float64) - 38)
+    v[::2] = 12 * torch.rand(len(v[::2]), generator=gen, dtype=torch.float64)
+    v[:4] = torch.tensor([float("inf"), float("inf"), 3.4028234e38, 3.4028234e38])
+    x, s = M.alloc_token_codes(rows, 1)
+    x.copy_((1 - 2 * (torch.arange(rows) % 2)).view(-1, 1))
+    s.copy_(v)
+    w, one = M.alloc_token_codes(1, 1)
+    w.fill_(1), one.fill_(1.0)
+    y = torch.empty(rows, 1, device="cuda")
+    h = M.mixaq_token_linear_create(w, one, None, act)
+    M.mixaq_token_linear_forward(h, x, y, x_scales=s)
+    torch.cuda.synchronize()
+    M.mixaq_token_linear_destroy(h)
+    v = s.double() * x[:, 0].double()
+    assert float(y[0]) == float("inf") and float(y[1]) == (-float("inf") if act == "none" else 0.0)
+    want, bound = R.activate(v[2:], torch.zeros_like(v[2:]), act)
+    R.check(y[2:], want[:, None], bound[:, None], "f32")
+
+
 def far(rows, cols, dtype, stride):
     """Rows whose offsets pass 2^32 bytes, in memory that is not filled."""
     return torch.empty(rows * stride, dtype=dtype, device="cuda").as_strided((rows, cols), (stride, 1))
