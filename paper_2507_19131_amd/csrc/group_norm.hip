@@ -38,71 +38,66 @@ __device__ __forceinline__ double shfl64(double v, int from)
     return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
 
-// Which rows and channels a thread takes: of up to 64 units a wave takes whole rows, 64 / units of them, of more the workgroup does.  slot < slots for threads that
-// take any; `left`: how many rows of sums there are once a wave has added up its own.
-struct Place { int u, slot, slots, of_wave, left; };
+// Which rows and channels a thread takes: slot < slots of those that take any.
+struct Place { int u, slot, slots; };
 template <int THREADS>
 __device__ __forceinline__ Place place_of(int units)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Place p;
-    if (units <= 64) {
-        p.of_wave = 64 / units;
-        const int s = lane / units;
-        p.u = lane - s * units;
-        p.slots = p.of_wave * (THREADS / 64);
-        p.slot = s < p.of_wave ? wave * p.of_wave + s : p.slots;
-        p.left = THREADS / 64;
-    } else {
-        p.of_wave = 1;
-        p.slots = p.left = THREADS / units;
-        p.slot = threadIdx.x / units;
-        p.u = threadIdx.x - p.slot * units;
-    }
+    p.slots = THREADS / units;
+    p.slot = threadIdx.x / units;
+    p.u = threadIdx.x - p.slot * units;
     return p;
 }
 
-// Adds up what the threads of a workgroup have for each group, of a unit's eight channels together (WHOLE) or each for itself: the rows of a wave by halves, then 16 lanes a
-// group the rows that are left.  One thread a group calls to(g, sums).  The order goes by the sizes alone.
+// Adds up what the threads of a workgroup have for each group, of a unit's eight channels together (WHOLE) or each for itself: of many rows of sums those that are `left`
+// apart, then 16 lanes a group the rows that are left.  (Exchanges between lanes in place of the first step pass LDS as well, and more often: 49 x 96 with three
+// channels a group 12.1 us instead of 7.2.)  One thread a group calls to(g, sums).  The order goes by the sizes alone.
 template <int THREADS, bool TINY, bool WHOLE, int E, typename To>
-__device__ __forceinline__ void add_up(double (&v)[E], double (&q)[E], const Place& p, int units, int per_group, int groups, int C, Sums (*red)[THREADS], To to)
+__device__ __forceinline__ void add_up(const double (&v)[E], const double (&q)[E], const Place& p, int units, int per_group, int groups, int C, Sums (*red)[THREADS], To to)
 {
-    const int lane = threadIdx.x & 63;
-    for (int n = p.of_wave; n > 1;) {                                        // (lanes without a row hold zeros and are nobody's upper half)
-        const int half = (n + 1) / 2, from = lane + half * units, upper = from < n * units;
+    constexpr int LANES = 16;
+    const int left = p.slots <= 2 * LANES ? p.slots : LANES * (p.slots >= 512 ? 8 : p.slots >= 128 ? 4 : 1);
+    if (p.slot < p.slots) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const double ov = shfl64(v[e], from), oq = shfl64(q[e], from);
-            v[e] += upper ? ov : 0.0;
-            q[e] += upper ? oq : 0.0;
-        }
-        n = half;
-    }
-    const int row = units <= 64 ? threadIdx.x >> 6 : p.slot;
-    if (p.slot < p.slots && (units > 64 || lane < units)) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) red[e][row * units + p.u] = {v[e], q[e]};
+        for (int e = 0; e < E; ++e) red[e][threadIdx.x] = {v[e], q[e]};
     }
     __syncthreads();
-    for (int g0 = 0; g0 < groups; g0 += THREADS / 16) {
-        const int g = g0 + threadIdx.x / 16, l = threadIdx.x & 15;
+    if (left < p.slots) {
+        const int row = left * units;
+        for (int i = threadIdx.x; i < E * row; i += THREADS) {               // (the only thread that reads or writes these rows of this channel)
+            const int e = E == 1 ? 0 : i / row;
+            Sums s = {0.0, 0.0};
+            for (int at = i - e * row; at < p.slots * units; at += row) {
+                s.v += red[e][at].v;
+                s.q += red[e][at].q;
+            }
+            red[e][i - e * row] = s;
+        }
+        __syncthreads();
+    }
+    const int lane = threadIdx.x & 63;
+    for (int g0 = 0; g0 < groups; g0 += THREADS / LANES) {
+        const int g = g0 + threadIdx.x / LANES, l = threadIdx.x % LANES;
         Sums s = {0.0, 0.0};
-        if (g < groups && l < p.left) {
+        if (g < groups) {
             auto more = [&](const Sums& o) {
                 s.v += o.v;
                 s.q += o.q;
             };
-            if constexpr (WHOLE) {
-                for (int i = g * (per_group / 8); i < (g + 1) * (per_group / 8); ++i) more(red[0][l * units + i]);
-            } else {
-                for (int i = g * per_group; i < (g + 1) * per_group; ++i) {
-                    const int unit = i / 8, at = place8<TINY>(unit * 8, C).at;
-                    more(red[i - at][l * units + unit]);
+            for (int r = l; r < left; r += LANES) {
+                if constexpr (WHOLE) {
+                    for (int i = g * (per_group / 8); i < (g + 1) * (per_group / 8); ++i) more(red[0][r * units + i]);
+                } else {
+                    for (int i = g * per_group; i < (g + 1) * per_group; ++i) {
+                        const int unit = i / 8, at = place8<TINY>(unit * 8, C).at;
+                        more(red[i - at][r * units + unit]);
+                    }
                 }
             }
         }
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) {
+        for (int d = 1; d < LANES; d <<= 1) {
             s.v += shfl64(s.v, lane ^ d);
             s.q += shfl64(s.q, lane ^ d);
         }
@@ -372,11 +367,10 @@ __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
 // Chunks of an image: a workgroup a CU in all (what every one adds up first grows with their number), each with rows for a turn of AHEAD or more.
 constexpr int THREADS = 512, MOST_THREADS_EACH = 1024;                       // of a workgroup, of one for more than 4096 channels
 int threads_of(int units) { return units > THREADS ? MOST_THREADS_EACH : THREADS; }
-int slots_of(int units, int threads) { return units <= 64 ? 64 / units * (threads / 64) : threads / units; }
 struct Chunks { int count, rows; };
 Chunks chunks_of(int rows, int images, int units)
 {
-    const int turn = slots_of(units, threads_of(units));
+    const int turn = threads_of(units) / units;
     const long long most = ((long long)rows + AHEAD * turn - 1) / (AHEAD * turn), wanted = std::max(1, (256 + images - 1) / images);
     const int count = (int)std::min(most, wanted), per = (rows + count - 1) / count;
     return {(rows + per - 1) / per, per};
@@ -410,7 +404,7 @@ int parts_of(const mixaq_group_norm_desc& d)
 {
     int width = d.C / d.groups;
     while (width % 8) width += d.C / d.groups;                               // (after at most eight)
-    if (d.C % 8 || d.C % width || width / 8 > 1024 || (d.rows_per_image - 1LL) / slots_of(width / 8, 1024) >= HELD) return 0;
+    if (d.C % 8 || d.C % width || width / 8 > 1024 || (d.rows_per_image - 1LL) / (1024 / (width / 8)) >= HELD) return 0;
     return d.C / width;
 }
 
