@@ -54,21 +54,22 @@ __device__ __forceinline__ Place place_of(int units)
 // apart, then 16 lanes a group the rows that are left.  (Exchanges between lanes in place of the first step pass LDS as well, and more often: 49 x 96 with three
 // channels a group 12.1 us instead of 7.2.)  One thread a group calls to(g, sums).  The order goes by the sizes alone.
 template <int THREADS, bool TINY, bool WHOLE, int E, typename To>
-__device__ __forceinline__ void add_up(const double (&v)[E], const double (&q)[E], const Place& p, int units, int per_group, int groups, int C, Sums (*red)[THREADS], To to)
+__device__ __forceinline__ void add_up(const double (&v)[E], const double (&q)[E], const Place& p, int units, int per_group, int groups, int C, Sums (*red)[THREADS * 9 / 8], To to)
 {
     constexpr int LANES = 16;
     const int left = p.slots <= 2 * LANES ? p.slots : LANES * (p.slots >= 512 ? 8 : p.slots >= 128 ? 4 : 1);
+    const int stride = units < 8 ? units : units | 1;                        // odd, so that the rows of a unit lie in different banks
     if (p.slot < p.slots) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) red[e][threadIdx.x] = {v[e], q[e]};
+        for (int e = 0; e < E; ++e) red[e][p.slot * stride + p.u] = {v[e], q[e]};
     }
     __syncthreads();
     if (left < p.slots) {
-        const int row = left * units;
+        const int row = left * stride;
         for (int i = threadIdx.x; i < E * row; i += THREADS) {               // (the only thread that reads or writes these rows of this channel)
             const int e = E == 1 ? 0 : i / row;
             Sums s = {0.0, 0.0};
-            for (int at = i - e * row; at < p.slots * units; at += row) {
+            for (int at = i - e * row; at < p.slots * stride; at += row) {
                 s.v += red[e][at].v;
                 s.q += red[e][at].q;
             }
@@ -87,11 +88,11 @@ __device__ __forceinline__ void add_up(const double (&v)[E], const double (&q)[E
             };
             for (int r = l; r < left; r += LANES) {
                 if constexpr (WHOLE) {
-                    for (int i = g * (per_group / 8); i < (g + 1) * (per_group / 8); ++i) more(red[0][r * units + i]);
+                    for (int i = g * (per_group / 8); i < (g + 1) * (per_group / 8); ++i) more(red[0][r * stride + i]);
                 } else {
                     for (int i = g * per_group; i < (g + 1) * per_group; ++i) {
                         const int unit = i / 8, at = place8<TINY>(unit * 8, C).at;
-                        more(red[i - at][r * units + unit]);
+                        more(red[i - at][r * stride + unit]);
                     }
                 }
             }
@@ -184,7 +185,7 @@ template <typename T, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int parts)
 {
     constexpr int E = WHOLE ? 1 : 8;
-    __shared__ Sums red[E][THREADS];
+    __shared__ Sums red[E][THREADS * 9 / 8];
     __shared__ Factors factor[8];                                            // (of lcm(8, per_group) channels)
     const int image = blockIdx.x / parts, part = blockIdx.x - image * parts, width = A.C / parts, units = width / 8;
     const Place p = place_of<THREADS>(units);
@@ -234,7 +235,7 @@ template <typename T, bool TINY, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_sums_kernel(GroupArgs A)
 {
     constexpr int E = WHOLE ? 1 : 8, TURN = AHEAD / (sizeof(T) == 4 ? 2 : 1) / (THREADS == 1024 ? 2 : 1);
-    __shared__ Sums red[E][THREADS];
+    __shared__ Sums red[E][THREADS * 9 / 8];
     const int image = blockIdx.x / A.chunks, chunk = blockIdx.x - image * A.chunks;
     const Place p = place_of<THREADS>(A.units);
     const int slots = p.slots, slot = p.slot;
