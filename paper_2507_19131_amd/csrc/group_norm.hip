@@ -179,7 +179,7 @@ __device__ __forceinline__ void store_values(const GroupArgs& A, long long row, 
 }
 
 // Small maps in one kernel: a workgroup holds its channels of an image, whole groups and whole units, in registers.  What bounds it: a launch, a round trip and the
-// reductions (1050 x 256 of f16 6.7 us of a graph replay, in the two kernels of larger maps 12).
+// reductions (1050 x 256 of f16 6.7 us of a graph replay; 4200 x 768, in the two kernels of larger maps, 12).
 constexpr int HELD = 4;                           // rows of a thread
 template <typename T, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int parts)
