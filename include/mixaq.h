@@ -380,7 +380,8 @@ typedef struct mixaq_token_linear mixaq_token_linear;
 int mixaq_token_linear_create(const mixaq_token_linear_desc *desc, const mixaq_token_linear_params *params, void *stream, mixaq_token_linear **out);
 int mixaq_token_linear_destroy(mixaq_token_linear *h);
 /* Bytes of device workspace that are enough for the calls below with an x of up to `x_rows` rows of this type (0: none, workspace may be NULL;
- * mixaq_token_linear_forward needs none for few rows of values either); a workspace is 256-byte aligned.  Calls that may overlap in time need workspaces of their own, captured ones included. */
+ * few rows of values need none either, which the calls decide by their own rows); a workspace is 256-byte aligned.  Calls that may overlap in time need
+ * workspaces of their own, captured ones included. */
 int mixaq_token_linear_workspace_bytes(const mixaq_token_linear *h, int32_t x_rows, int32_t x_type, size_t *bytes);
 /* Allocates nothing and does not wait; may be captured.  The memory of x, y and workspace must not overlap.  The handle is not
  * changed: calls on any streams of its device, which has to be current, may share it. */

@@ -6,11 +6,17 @@ namespace mixaq {
 
 enum TokenForm { TOKEN_FEW, TOKEN_MID, TOKEN_SPLIT, TOKEN_TILE, TOKEN_WIDE };
 
-// Whether values are quantized on their way into FEW's product: every workgroup looks for the maxima of its 16 whole rows, so only where a wave has one block of K
-// and workgroups are few.  us of graph replays, bf16 / f32 values, in one launch and in two (the second takes the host another 3.5):
-//     1 x 1024 x 4096 4.0 / 5.0, 3.8 / 5.0    16 x 1024 x 4096 4.5 / 5.7, 5.3 / 5.7    64 x 1024 x 1024 4.5 / 5.7, 5.3 / 6.2 |  32 x 1024 x 4096 6.0 / 6.3,
-//     7.3 / 6.4    1 x 4096 x 4096 7.4 / 5.9, 7.2 / 6.0    16 x 4096 x 1024 10.0 / 7.3, 16.0 / 7.3
-inline bool token_quantized_inside(int M, int KB, int NB) { return KB <= 8 && (M + 15LL) / 16 * NB * 8 <= 256; }
+// Whether values of M rows are quantized on their way into FEW's product: every workgroup quantizes its 16 whole rows for itself, so only rows of no more than it holds
+// and few workgroups.  us of graph replays, bf16 / f32 values, in one launch and in two (the second takes the host another 3.5 where nothing is captured):
+//   512 of 16 outputs: 1 x 1024 x 4096 (256) 4.3 / 5.1, 4.3 / 5.0    64 x 1024 x 1024 (256) 4.5 / 5.7, 4.6 / 6.2    32 x 1024 x 4096 (512) 5.5 / 6.4, 5.5 / 6.4
+//     128 x 1024 x 1024 (512) 5.5 / 6.4, 5.5 / 6.4    16 x 1024 x 8192 (512) 5.4 / 6.3, 5.4 / 6.2 |  64 x 1024 x 4096 (1024) 7.9 / 7.9, 7.9 / 7.8
+//   Rows sorted by expert, up to 64 in 1024 of 64 outputs (K x N of experts): 16 of 1024 x 2048 of 32 (1024) 7.7 / 7.8, 7.9 / 7.8    64 the same 12.8 / 13.2, 12.9 / 13.4
+//     64 of 512 x 1024 of 8 (128) 5.1 / 6.1, 5.0 / 6.0 |  128 of 512 x 1024 of 8 7.6 / 7.3, 7.4 / 7.2    16 of 1024 x 4096 of 128 (8192) 17.8 / 16.3, 17.6 / 16.2
+inline bool token_quantized_inside(int M, int K, int NB, int experts, bool sorted)
+{
+    if (K < 8 || K > 1024) return false;                                     // (rows of fewer than 8 values have no eight to load)
+    return sorted ? M <= 64 && M / experts <= 16 && (long long)experts * NB * 2 <= 1024 : (M + 15LL) / 16 * NB * 8 <= 512;
+}
 
 // M rows, KB and NB blocks of 128 inputs and outputs; reach: bytes from the first row of codes that a tile may read to behind the last.  us of graph replays, to bf16:
 //   FEW, 16 rows by eight waves, 16 outputs, or 64 where those would be over 1024 workgroups.  MID, 32 x 32 by eight waves, where FEW would be over 512 workgroups and

@@ -82,49 +82,24 @@ __device__ __forceinline__ int source_of(const TokenArgs& A, int r)
 
 // ---- operands straight from memory, K split over the waves --------------------------------------------------------------------
 // A workgroup of NW waves computes 16 MR rows times NR tiles of 16 outputs, wave w the blocks w, w + NW, .. of K; the waves' sums meet in LDS.
-// x may be given as values: the waves look for the rows' maxima first, each in its blocks, and quantize what they multiply.  SORTED: a workgroup takes
-// all rows of its expert, one tile after the other, so that weights come once.  Weights, rows, scales and bias are asked for as soon as their places are known.
-// What bounds it: a launch and round trips to memory (1 x 1024 x 4096 from codes 3.1 us of a graph replay, 4.2 MB of weights would take 0.8; from values 4.0; 16 rows of
+// x may be given as values (8 .. INSIDE_K a row): the workgroup quantizes its 16 rows into LDS first, 32 lanes a row, a row in registers between its maximum
+// and its codes.  SORTED: a workgroup takes all rows of its expert, one tile after the other, so that weights come once.  Weights, rows, scales and bias are asked
+// for as soon as their places are known.
+// What bounds it: a launch and round trips to memory (1 x 1024 x 4096 from codes 3.1 us of a graph replay, 4.2 MB of weights would take 0.8; from values 4.3; 16 rows of
 // 32 experts, 2048 x 1024 each, 5.6 us where the 27 MB of the experts they hit take 5.4), with more rows the operands' way through the caches, each workgroup
 // for itself (256 x 1024 x 1024 in 32 x 32 4.2 us, 1024 x 4096 x 1024 in 64 x 64 14.7).
-template <typename T>
-__device__ __forceinline__ void values_of(const T* from, int k0, int K, T (&t)[2][16])        // 16 from k0 on, 16 from k0 + 64 on
-{
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int k = k0 + h * 64;
-        if (k + 16 <= K) __builtin_memcpy(t[h], from + k, sizeof(t[h]));
-        else
-#pragma unroll
-            for (int e = 0; e < 16; ++e) t[h][e] = k + e < K ? from[k + e] : (T)0.0f;
-    }
-}
-template <typename T>
-__device__ __forceinline__ unsigned largest_of(const T (&t)[2][16])
-{
-    unsigned m = 0;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) m = max(m, magnitude((float)t[e >> 4][e & 15]));
-    return m;
-}
-template <typename T>
-__device__ __forceinline__ void operands_of(const T (&t)[2][16], float inv, v4i (&x)[2])
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const T* const f = &t[i >> 2][4 * (i & 3)];
-        x[i >> 2][i & 3] = int_codes4((float)f[0], (float)f[1], (float)f[2], (float)f[3], inv);
-    }
-}
+constexpr int INSIDE_K = 1024;                    // the most inputs of values that are quantized here
 
 template <int XT, int YT, int MR, int NR, int NW, bool SORTED>
-__global__ __launch_bounds__(NW * 64, XT == MIXAQ_I8 && MR == 1 ? 4 : 1) void token_few_kernel(TokenArgs A, int per, FastDiv by_per, int groups)
+__global__ __launch_bounds__(NW * 64, MR == 1 ? 4 : 1) void token_few_kernel(TokenArgs A, int per, FastDiv by_per, int groups)
 {
     constexpr int FR = MR * NR;                                              // 16 x 16 results of the workgroup
     constexpr bool FROM_CODES = XT == MIXAQ_I8;
     using X = typename std::conditional<FROM_CODES, TypeOf<MIXAQ_E4M3>, TypeOf<XT>>::type::T;
     __shared__ v4i part[NW][FR][64];
-    __shared__ unsigned top[NW][16 * MR];
+    constexpr int CODED = FROM_CODES ? 16 : INSIDE_K + 16;                   // bytes of a row of codes: 16 lanes of a chunk in different banks
+    __shared__ v4i coded[16][CODED / 16];
+    static_assert(FROM_CODES || (MR == 1 && NW * 64 == 16 * 32 && NW * SBLOCK >= INSIDE_K), "16 rows, a block of K for each wave");
     __shared__ float scale_of[16 * MR];
     __shared__ int source[16 * MR];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
@@ -150,9 +125,6 @@ __global__ __launch_bounds__(NW * 64, XT == MIXAQ_I8 && MR == 1 ? 4 : 1) void to
     }
     struct Operands { v4i w[NR][2], x[MR][2]; };
     for (int r0 = first; r0 < (SORTED ? end : first + 1); r0 += 16 * MR) {
-        const X* from[MR];
-        int src[MR];
-        RowScale s[MR];
         auto load_w = [&](int kb, Operands& o) {
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
@@ -160,58 +132,55 @@ __global__ __launch_bounds__(NW * 64, XT == MIXAQ_I8 && MR == 1 ? 4 : 1) void to
                 o.w[n][1] = w0[(kb * 8 + n) * 128 + 64];
             }
         };
+        Operands now;
+        const bool works = wave < A.KB;
+        if (FROM_CODES && works) load_w(wave, now);                          // on their way while the rows are looked up
+        const X* from[MR];
         auto load_x = [&](int kb, Operands& o) {                             // (behind a row's end the row's first codes: the weights there are zero)
             const int k0 = kb * SBLOCK + g * 16;
 #pragma unroll
             for (int m = 0; m < MR; ++m) {
-                if constexpr (FROM_CODES) {
-                    o.x[m][0] = *(const v4i*)(from[m] + (k0 < A.K ? k0 : 0));
-                    o.x[m][1] = *(const v4i*)(from[m] + (k0 + 64 < A.K ? k0 + 64 : 0));
-                } else {
-                    X t[2][16];
-                    values_of(from[m], k0, A.K, t);
-                    operands_of(t, s[m].inv, o.x[m]);
-                }
+                o.x[m][0] = *(const v4i*)(from[m] + (k0 < A.K ? k0 : 0));
+                o.x[m][1] = *(const v4i*)(from[m] + (k0 + 64 < A.K ? k0 + 64 : 0));
             }
         };
-        Operands now;
-        const bool works = wave < A.KB;
-        if (works) load_w(wave, now);                                        // on their way while the rows are looked up
-#pragma unroll
-        for (int m = 0; m < MR; ++m) {
-            const int r = min(r0 + m * 16 + c, end - 1);
-            src[m] = SORTED ? source_of(A, r) : r;
-            from[m] = (const X*)A.x + (long long)max(src[m], 0) * A.ldx;
-        }
         if constexpr (FROM_CODES) {
 #pragma unroll
-            for (int m = 0; m < MR; ++m) s[m].scale = A.sx[max(src[m], 0)];
+            for (int m = 0; m < MR; ++m) {
+                const int r = r0 + m * 16 + c, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
+                from[m] = (const X*)A.x + (long long)max(src, 0) * A.ldx;
+                if (wave == 0 && g == 0) {
+                    scale_of[m * 16 + c] = A.sx[max(src, 0)];
+                    source[m * 16 + c] = r < end ? src : -1;
+                }
+            }
             if (works) load_x(wave, now);
         } else {
-            X t[MR][2][16];                                                  // the first block stays in registers until its row's scale is known
+            const int row = threadIdx.x >> 5, l = threadIdx.x & 31, r = r0 + row, at = min(r, end - 1), src = SORTED ? source_of(A, at) : at;
+            const X* const values = (const X*)A.x + (long long)max(src, 0) * A.ldx;
+            Eight place[INSIDE_K / 256];
+            float v[INSIDE_K / 256][8];
+            unsigned largest = 0;
 #pragma unroll
-            for (int m = 0; m < MR; ++m) {
-                unsigned largest = 0;
-                if (works) {
-                    values_of(from[m], wave * SBLOCK + g * 16, A.K, t[m]);
-                    largest = largest_of(t[m]);
-                }
-                for (int kb = wave + NW; kb < A.KB; kb += NW) {
-                    X u[2][16];
-                    values_of(from[m], kb * SBLOCK + g * 16, A.K, u);
-                    largest = max(largest, largest_of(u));
-                }
-                largest = over4rows(largest, MaxOf());
-                if (g == 0) top[wave][m * 16 + c] = largest;
+            for (int j = 0; j < INSIDE_K / 256; ++j) {
+                place[j] = place8<false>((j * 32 + l) * 8, A.K);
+                load8f<false>(values, place[j], A.K, v[j]);
+            }
+            if (works) load_w(wave, now);                                    // (behind the values: loads come back in order)
+#pragma unroll
+            for (int j = 0; j < INSIDE_K / 256; ++j) largest = max(largest, max_magnitude<false>(place[j], A.K, v[j]));
+            largest = max16(largest);
+            const RowScale s = row_scale(max(largest, (unsigned)__shfl_xor((int)largest, 16, 64)));
+#pragma unroll
+            for (int j = 0; j < INSIDE_K / 256; ++j) store_int_codes8<false>((int8_t*)coded[row], place[j], A.K, v[j], s.inv);
+            if (l == 0) {
+                scale_of[row] = s.scale;
+                source[row] = r < end ? src : -1;
             }
             __syncthreads();
-#pragma unroll
-            for (int m = 0; m < MR; ++m) {
-                unsigned largest = 0;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) largest = max(largest, top[w][m * 16 + c]);
-                s[m] = row_scale(largest);
-                if (works) operands_of(t[m], s[m].inv, now.x[m]);
+            if (works) {                                                     // (what stands behind a row's end: the weights there are zero)
+                now.x[0][0] = coded[c][wave * 8 + g];
+                now.x[0][1] = coded[c][wave * 8 + g + 4];
             }
         }
         v4i acc[MR][NR] = {};
@@ -225,7 +194,7 @@ __global__ __launch_bounds__(NW * 64, XT == MIXAQ_I8 && MR == 1 ? 4 : 1) void to
                 }
         };
         if (works) {                                                         // one block's operands travel under the products of the last one
-            for (int kb = wave + NW; kb < A.KB; kb += NW) {
+            for (int kb = wave + NW; FROM_CODES && kb < A.KB; kb += NW) {
                 Operands next;
                 load_w(kb, next);
                 load_x(kb, next);
@@ -235,14 +204,9 @@ __global__ __launch_bounds__(NW * 64, XT == MIXAQ_I8 && MR == 1 ? 4 : 1) void to
             multiply(now);
         }
 #pragma unroll
-        for (int m = 0; m < MR; ++m) {
+        for (int m = 0; m < MR; ++m)
 #pragma unroll
             for (int n = 0; n < NR; ++n) part[wave][m * NR + n][lane] = acc[m][n];
-            if (wave == 0 && g == 0) {
-                scale_of[m * 16 + c] = s[m].scale;
-                source[m * 16 + c] = r0 + m * 16 + c < end ? src[m] : -1;
-            }
-        }
         __syncthreads();
         using T = typename TypeOf<YT>::T;
         const int used = min(NW, A.KB);
@@ -671,11 +635,10 @@ int launch_linear(const TokenArgs& A, TokenForm form, int x_type, const mixaq_ro
     case TOKEN_SPLIT: return launch_few<MIXAQ_I8, YT, 4, 4, 4, SORTED>(A, values, st);
     case TOKEN_FEW: break;
     }
-    if constexpr (!SORTED) {
-        if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT, 1, 1, 8, SORTED>(A, nullptr, st);
-        if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT, 1, 1, 8, SORTED>(A, nullptr, st);
-        if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT, 1, 1, 8, SORTED>(A, nullptr, st);
-    }
+    constexpr int NR = SORTED ? 4 : 1;                                       // of values
+    if (x_type == MIXAQ_F32) return launch_few<MIXAQ_F32, YT, 1, NR, 8, SORTED>(A, nullptr, st);
+    if (x_type == MIXAQ_F16) return launch_few<MIXAQ_F16, YT, 1, NR, 8, SORTED>(A, nullptr, st);
+    if (x_type == MIXAQ_BF16) return launch_few<MIXAQ_BF16, YT, 1, NR, 8, SORTED>(A, nullptr, st);
     // 16 outputs a workgroup, or 64 where those would be more than run at one time
     if ((SORTED ? A.experts : (A.M + 15LL) / 16) * A.NB * 8 > 1024) return launch_few<MIXAQ_I8, YT, 1, 4, 8, SORTED>(A, values, st);
     return launch_few<MIXAQ_I8, YT, 1, 1, 8, SORTED>(A, values, st);
@@ -755,7 +718,7 @@ int forward(const mixaq_token_linear* h, const mixaq_rows* x, int32_t x_rows, co
     HIP_TRY(hipGetDevice(&device));
     if (device != h->device) return fail(MIXAQ_E_SHAPE, "the layer was created on device %d, device %d is current", h->device, device);
     mixaq_rows codes = *x;
-    const size_t need = !sorted && token_quantized_inside(x_rows, h->KB, h->NB) ? 0 : workspace_of(h, x_rows, x->type);
+    const size_t need = token_quantized_inside(rows, K, h->NB, h->d.experts, sorted != nullptr) ? 0 : workspace_of(h, x_rows, x->type);
     if (need) {
         if (!workspace) return fail(MIXAQ_E_NULL, "workspace is NULL (%zu bytes needed)", need);
         if (workspace_bytes < need) return fail(MIXAQ_E_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);

@@ -325,6 +325,31 @@ def test_gathered_and_weighted(experts, tokens, choices, K, N, x_kind):
         check_sorted(layer, codes, scales, counts, 0, y, "f32", gather, weights)
 
 
+@pytest.mark.parametrize("x_kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("before", [0, 3])
+@pytest.mark.parametrize("rows,K,N", [(1, 1, 1), (33, 7, 130), (33, 8, 40), (64, 9, 64), (5, 1017, 65), (64, 1024, 300), (64, 1025, 300), (65, 1024, 100)])
+def test_few_sorted_rows_of_values_are_their_codes(rows, K, N, before, x_kind):
+    """On both sides of where values are quantized on their way in; most rows to one expert, more than a tile of them."""
+    counts = [1, 0, rows - 1, 0, 0, 0]
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    gather = torch.randint(0, rows, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    gather[3::11] = -1
+    with Layer(rows + K, N, K, 6, "silu") as layer:
+        x = placed(values(rows, rows, K), x_kind, before, 0)
+        q = placed(values(rows, rows, K), "i8")
+        codes, scales = R.quantize(x.t)
+        q.t.copy_(codes)
+        a, b = Room(rows, N, "f32"), Room(rows, N, "f32")
+        if S.inside(rows, K, N, 6):
+            M.mixaq_token_linear_forward_grouped(layer.h, x.t, offsets_of(counts), a.t, gather=gather)        # without a workspace
+        else:
+            layer.grouped(x.t, offsets_of(counts), a.t, gather=gather)
+        layer.grouped(q.t, offsets_of(counts), b.t, scales, gather=gather)
+        R.same(a.t, b.t)
+        check_sorted(layer, codes, scales, counts, 0, a, "f32", gather)
+        assert x.untouched()
+
+
 @pytest.mark.parametrize("rows", [10, 3000])
 def test_offsets_that_are_no_offsets(rows):
     """Beyond the rows they are cut off; falling ones leave rows undefined, and nothing outside the rows is read or written."""

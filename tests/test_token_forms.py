@@ -28,9 +28,16 @@ def test_rows_sorted_by_expert():
 
 
 def test_values_are_quantized_inside_in_few_rows_alone():
-    assert S.inside(16, 1024, 4096) and not S.inside(17, 1024, 4096) and not S.inside(1, 1025, 128) and S.inside(512, 1024, 128)
+    assert S.inside(32, 1024, 4096) and not S.inside(33, 1024, 4096) and not S.inside(1, 1025, 128) and S.inside(1024, 1024, 128)
+    assert S.inside(1, 8, 128) and not S.inside(1, 7, 128) and S.inside(1, 1024, 8192) and not S.inside(1, 1024, 8193)
+    assert S.inside(64, 1024, 2048, 32) and not S.inside(65, 1024, 2048, 32) and not S.inside(64, 1024, 2049, 32) and not S.inside(64, 1024, 2048, 33)
+    assert S.inside(64, 1024, 100, 4) and not S.inside(64, 1024, 100, 3) and S.inside(16, 1024, 100, 1) and not S.inside(17, 1024, 100, 1)
+    assert not S.inside(1, 1024, 1 << 12, 1 << 12)
     for rows, K, N in S.SIZES:
         assert not S.inside(rows, K, N) or S.form(rows, K, N) == "few"
+    for experts, rows, K, N, _ in S.SORTED:
+        assert not S.inside(rows, K, N, experts) or S.form(rows, K, N, experts) == "few"
+    assert any(S.inside(rows, K, N, experts) for experts, rows, K, N, _ in S.SORTED)
 
 
 @pytest.mark.parametrize("sizes,experts", [(S.SIZES, False), (S.SORTED, True)])

@@ -11,7 +11,7 @@ NAMES = ("few", "mid", "split", "tile", "wide")
 _SOURCE = r'''
 #include "token_forms.h"
 extern "C" int form(int M, int KB, int NB, int experts, int sorted, long long reach) { return mixaq::token_form(M, KB, NB, experts, sorted, reach); }
-extern "C" int inside(int M, int KB, int NB) { return mixaq::token_quantized_inside(M, KB, NB); }
+extern "C" int inside(int M, int K, int NB, int experts, int sorted) { return mixaq::token_quantized_inside(M, K, NB, experts, sorted); }
 '''
 
 
@@ -39,9 +39,9 @@ def form(rows, K, N, experts=0, stride=None):
     return NAMES[lib.form(rows, blocks(K), blocks(N), max(experts, 1), experts > 0, stride * (rows if experts else 128))]
 
 
-def inside(rows, K, N):
+def inside(rows, K, N, experts=0):
     """Whether values are quantized on their way into the product."""
-    return bool(lib.inside(rows, blocks(K), blocks(N)))
+    return bool(lib.inside(rows, K, blocks(N), max(experts, 1), experts > 0))
 
 
 # rows, K, N: K that ends inside 16 codes, a step of 32, a stage of 64 and a block; outputs that end inside 16, 64 and 128, an odd number of blocks
