@@ -391,14 +391,15 @@ int mixaq_token_linear_forward(const mixaq_token_linear *h, const mixaq_rows *x,
  * offsets: device int32 [experts + 1], rising, read by the kernels and never by the host: rows may be shared out anew in a captured graph.  What
  * lies outside 0 .. rows is cut off; falling offsets leave the rows between them undefined.  gather: device int32 [rows], the row of x that
  * row r reads, or NULL (row r; then x_rows >= rows); a row whose index lies outside 0 .. x_rows - 1 is left as it was, and so are rows of y
- * outside offsets[0] .. offsets[experts] - 1.  row_weights: device float [rows] or NULL (1).  x has x_rows rows and is quantized once a row, however often
- * gather names it.  rows: of y; the list and the weights are as long.  y must overlap none of the other arguments. */
+ * outside offsets[0] .. offsets[experts] - 1.  row_weights: device float [rows] or NULL (1).  x has x_rows rows; its values are quantized row by row, as
+ * above, whatever names them.  rows: of y; the list and the weights are as long.  y must overlap none of the other arguments. */
 int mixaq_token_linear_forward_grouped(const mixaq_token_linear *h, const mixaq_rows *x, int32_t x_rows, const int32_t *offsets, const int32_t *gather,
                                        const float *row_weights, const mixaq_rows *y, int32_t rows, void *workspace, size_t workspace_bytes, void *stream);
 
 /* y = act((x - mean) / sqrt(variance + eps) * gamma + beta) on a batch of channels-last maps: x [images * rows_per_image, C] as the blocks and
  * layers here leave them, the mean and the (biased) variance those of the C / groups neighbouring channels of all rows of an image.  Sums are taken in
- * binary64, the rest in binary32.  gamma, beta: device float [C] or NULL (1, 0).  A group that holds a NaN or an infinity becomes NaN. */
+ * binary64, the rest in binary32 (a difference from the mean of 2^128 or more is an infinity).  gamma, beta: device float [C] or NULL (1, 0).  A group that
+ * holds a NaN or an infinity becomes NaN. */
 typedef struct {
     int32_t C, groups;        /* 1 .. 8192 channels; groups: at most 1024, a divisor of C         */
     int32_t rows_per_image;   /* 1 .. 2^30                                                        */

@@ -86,7 +86,8 @@ __device__ __forceinline__ int source_of(const TokenArgs& A, int r)
 // and its codes.  SORTED: a workgroup takes all rows of its expert, one tile after the other, so that weights come once.  Weights, rows, scales and bias are asked
 // for as soon as their places are known.
 // What bounds it: a launch and round trips to memory (1 x 1024 x 4096 from codes 3.1 us of a graph replay, 4.2 MB of weights would take 0.8; from values 4.3; 16 rows of
-// 32 experts, 2048 x 1024 each, 5.6 us where the 27 MB of the experts they hit take 5.4), with more rows the operands' way through the caches, each workgroup
+// 32 experts, 2048 x 1024 each, 5.6 us where the 27 MB of the experts they hit take 5.4; from values 7.7: a row comes after its offsets and its place in the list,
+// and the weights behind it, in whose place they would be waited for first), with more rows the operands' way through the caches, each workgroup
 // for itself (256 x 1024 x 1024 in 32 x 32 4.2 us, 1024 x 4096 x 1024 in 64 x 64 14.7).
 constexpr int INSIDE_K = 1024;                    // the most inputs of values that are quantized here
 
