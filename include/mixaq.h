@@ -407,6 +407,7 @@ typedef struct {
     float   eps;              /* > 0                                                              */
 } mixaq_group_norm_desc;
 typedef struct { const float *gamma, *beta; } mixaq_group_norm_params;
+/* Bytes of device workspace, 256-byte aligned, that are enough for calls of up to `rows` rows; a call of any size needs one. */
 int mixaq_group_norm_workspace_bytes(const mixaq_group_norm_desc *desc, int32_t rows, size_t *bytes);
 /* x: values.  y: values, or codes as mixaq_token_quantize makes them of the binary32 results.  rows: a multiple of rows_per_image, or 0.  y may be x itself
  * (same data, stride and type); apart from that the memory of y and of the workspace overlaps no other argument.  Allocates nothing and does not

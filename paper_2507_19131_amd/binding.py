@@ -739,6 +739,7 @@ def alloc_token_linear_workspace(h, x_rows, x_dtype, device="cuda:0"):
 
 
 def alloc_group_norm_workspace(norm, rows, device="cuda:0"):
+    """Enough for calls of up to `rows` rows."""
     return torch.empty(mixaq_group_norm_workspace_bytes(norm, rows), dtype=torch.uint8, device=device)
 
 

@@ -369,11 +369,15 @@ __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
 constexpr int THREADS = 512, MOST_THREADS_EACH = 1024;                       // of a workgroup, of one for more than 4096 channels
 int threads_of(int units) { return units > THREADS ? MOST_THREADS_EACH : THREADS; }
 struct Chunks { int count, rows; };
-Chunks chunks_of(int rows, int images, int units)
+long long most_chunks(int rows, int units)                                   // of an image
 {
     const int turn = threads_of(units) / units;
-    const long long most = ((long long)rows + AHEAD * turn - 1) / (AHEAD * turn), wanted = std::max(1, (256 + images - 1) / images);
-    const int count = (int)std::min(most, wanted), per = (rows + count - 1) / count;
+    return ((long long)rows + AHEAD * turn - 1) / (AHEAD * turn);
+}
+Chunks chunks_of(int rows, int images, int units)
+{
+    const long long wanted = std::max(1, (256 + images - 1) / images);
+    const int count = (int)std::min(most_chunks(rows, units), wanted), per = (rows + count - 1) / count;
     return {(rows + per - 1) / per, per};
 }
 
@@ -398,7 +402,14 @@ size_t sums_bytes(const mixaq_group_norm_desc& d, int images)
 {
     return (size_t)images * chunks_of(d.rows_per_image, images, units_of(d.C)).count * d.groups * sizeof(Sums);
 }
-size_t workspace_of(const mixaq_group_norm_desc& d, int images) { return images ? sums_bytes(d, images) + (size_t)images * d.groups * sizeof(float) : 0; }
+// What a call uses.
+size_t needed(const mixaq_group_norm_desc& d, int images) { return sums_bytes(d, images) + (size_t)images * d.groups * sizeof(float); }
+// Enough for up to `images`: the chunks of all of them rise and fall with their number (256 of 4 images, 258 of 3), but are never more than images + 255.
+size_t workspace_of(const mixaq_group_norm_desc& d, int images)
+{
+    const size_t chunks = (size_t)std::min(images * most_chunks(d.rows_per_image, units_of(d.C)), images + 255LL);
+    return images ? chunks * d.groups * sizeof(Sums) + (size_t)images * d.groups * sizeof(float) : 0;
+}
 
 // Of how many parts an image's channels are, whole groups and whole units of eight each, where a workgroup holds the rows of one; 0 where none does.
 int parts_of(const mixaq_group_norm_desc& d)
@@ -459,7 +470,7 @@ int mixaq_group_norm(const mixaq_group_norm_desc* desc, const mixaq_group_norm_p
     if (!rc) rc = check_token_rows(y, "y", d.C, VALUES | CODES);
     if (rc) return rc;
     const int images = rows / d.rows_per_image;
-    const size_t need = workspace_of(d, images);
+    const size_t need = needed(d, images);
     if (!workspace) return fail(MIXAQ_E_NULL, "workspace is NULL (%zu bytes needed)", need);
     if (workspace_bytes < need) return fail(MIXAQ_E_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     if ((uintptr_t)workspace & 255) return fail(MIXAQ_E_WORKSPACE, "workspace must be 256-byte aligned");
