@@ -409,7 +409,8 @@ typedef struct {
 typedef struct { const float *gamma, *beta; } mixaq_group_norm_params;
 /* Bytes of device workspace, 256-byte aligned, that are enough for calls of up to `rows` rows; a call of any size needs one. */
 int mixaq_group_norm_workspace_bytes(const mixaq_group_norm_desc *desc, int32_t rows, size_t *bytes);
-/* x: values.  y: values, or codes as mixaq_token_quantize makes them of the binary32 results.  rows: a multiple of rows_per_image, or 0.  y may be x itself
+/* x: values.  y: values, or codes as mixaq_token_quantize makes them of the binary32 results.  rows: a multiple of rows_per_image, or 0, of fewer than 2^23
+ * images (2^22 of more than 4096 channels): more than a launch holds are refused.  y may be x itself
  * (same data, stride and type); apart from that the memory of y and of the workspace overlaps no other argument.  Allocates nothing and does not
  * wait; may be captured; calls that may overlap in time need workspaces of their own. */
 int mixaq_group_norm(const mixaq_group_norm_desc *desc, const mixaq_group_norm_params *params, const mixaq_rows *x, const mixaq_rows *y, int32_t rows,

@@ -411,13 +411,14 @@ size_t workspace_of(const mixaq_group_norm_desc& d, int images)
     return images ? chunks * d.groups * sizeof(Sums) + (size_t)images * d.groups * sizeof(float) : 0;
 }
 
-// Of how many parts an image's channels are, whole groups and whole units of eight each, where a workgroup holds the rows of one; 0 where none does.
-int parts_of(const mixaq_group_norm_desc& d)
+// Of how many parts an image's channels are, whole groups and whole units of eight each, where a workgroup holds the rows of one; 0 where none does, or where the
+// workgroups of all images are more than a launch takes.
+int parts_of(const mixaq_group_norm_desc& d, int images)
 {
     int width = d.C / d.groups;
     while (width % 8) width += d.C / d.groups;                               // (after at most eight)
     if (d.C % 8 || d.C % width || width / 8 > 1024 || (d.rows_per_image - 1LL) / (1024 / (width / 8)) >= HELD) return 0;
-    return d.C / width;
+    return (long long)images * (d.C / width) * 1024 < MOST_THREADS ? d.C / width : 0;
 }
 
 template <typename T>
@@ -502,9 +503,9 @@ int mixaq_group_norm(const mixaq_group_norm_desc* desc, const mixaq_group_norm_p
     A.by_group = FastDiv(A.per_group);
     A.part = (Sums*)workspace;
     A.pivots = (float*)((char*)workspace + sums_bytes(d, images));
-    const int parts = y->type == MIXAQ_I8 ? 0 : parts_of(d);
+    const int parts = y->type == MIXAQ_I8 ? 0 : parts_of(d, images);
     const long long blocks = (long long)images * (parts ? parts : ch.count);
-    if (blocks * 1024 >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d images are too many for one call", images);
+    if (blocks * (parts ? 1024 : threads_of(A.units)) >= MOST_THREADS) return fail(MIXAQ_E_SHAPE, "%d images are too many for one call", images);
     if (x->type == MIXAQ_F32) launch_type<MIXAQ_F32>(A, parts, (unsigned)blocks, (hipStream_t)stream);
     else if (x->type == MIXAQ_F16) launch_type<MIXAQ_F16>(A, parts, (unsigned)blocks, (hipStream_t)stream);
     else launch_type<MIXAQ_BF16>(A, parts, (unsigned)blocks, (hipStream_t)stream);
