@@ -276,7 +276,8 @@ int mixaq_downsample_forward_taps(const mixaq_downsample *h, const float *x, flo
  * shorter) row r's scale is scales[b * scale_stride + r], and the values that codes stand for are code * scale.  Values may
  * start at any multiple of their size and have any stride >= columns.  Codes and their stride are multiples of 16 bytes, and every row
  * of a layer's x (the last one too) has room for its columns rounded up to 16: those bytes are read, what they hold changes nothing, and
- * nothing is ever written behind a row's columns.  Calls take 0 .. 2^30 rows; of no rows nothing is read, the pointers included. */
+ * nothing is ever written behind a row's columns.  Calls take 0 .. 2^30 rows, as far as a launch of 2^32 threads does (others are refused); of no rows
+ * nothing is read, the pointers included. */
 typedef enum { MIXAQ_F32 = 0, MIXAQ_F16 = 1, MIXAQ_BF16 = 2, MIXAQ_E4M3 = 3, MIXAQ_I8 = 4 /* the token calls below only */ } mixaq_type;
 typedef struct {
     void    *data;
@@ -360,8 +361,8 @@ int mixaq_residual_norm(const mixaq_residual_norm_desc *desc, const mixaq_residu
  * q: codes; they must not overlap.  rows may be 0. */
 int mixaq_token_quantize(const mixaq_rows *x, int32_t rows, int32_t columns, const mixaq_rows *q, void *stream);
 
-/* y = act(x w^T + bias) on codes of x [rows, K] and of w [N, K]: act(fma(sum_k c_x c_w, s_x s_w, bias)) in binary32, the sum exact, one rounding to
- * y's type at the end.  x may be given as values: they are quantized first, as mixaq_token_quantize does, with the same result.  y: values.
+/* y = act(x w^T + bias) on codes of x [rows, K] and of w [N, K]: act(fma(f32(sum_k c_x c_w), f32(s_x s_w), bias)), the sum exact in whole numbers and then the
+ * nearest binary32 value (itself up to 2^24), one rounding to y's type at the end.  Where s_x s_w passes binary32 results are infinite, of a sum of 0 NaN.  x may be given as values: they are quantized first, as mixaq_token_quantize does, with the same result.  y: values.
  * With `experts` above 1 the layer holds as many matrices and biases, [experts * N] rows one behind the other, and only
  * mixaq_token_linear_forward_grouped takes it. */
 typedef struct {
@@ -398,8 +399,8 @@ int mixaq_token_linear_forward_grouped(const mixaq_token_linear *h, const mixaq_
 
 /* y = act((x - mean) / sqrt(variance + eps) * gamma + beta) on a batch of channels-last maps: x [images * rows_per_image, C] as the blocks and
  * layers here leave them, the mean and the (biased) variance those of the C / groups neighbouring channels of all rows of an image.  Sums are taken in
- * binary64, the rest in binary32 (a difference from the mean of 2^128 or more is an infinity).  gamma, beta: device float [C] or NULL (1, 0).  A group that
- * holds a NaN or an infinity becomes NaN. */
+ * binary64, the rest in binary32 (a difference from the mean of 2^128 or more is an infinity, and so is gamma / sqrt(variance + eps)).  gamma, beta: device
+ * float [C] or NULL (1, 0).  A group that holds a NaN or an infinity becomes NaN. */
 typedef struct {
     int32_t C, groups;        /* 1 .. 8192 channels; groups: at most 1024, a divisor of C         */
     int32_t rows_per_image;   /* 1 .. 2^30                                                        */
