@@ -229,8 +229,9 @@ __global__ __launch_bounds__(THREADS) void group_small_kernel(GroupArgs A, int p
 constexpr int AHEAD = 8;                          // rows of a thread that are on their way at one time (of 32 bits half as many)
 
 // The sums of one chunk of rows.  A thread keeps to eight channels, so that the threads of a workgroup read whole rows one behind the other.  WHOLE: a
-// group is a multiple of eight channels, whose sums a thread takes together.  What bounds it is memory: 4 x 65536 x 128 of bf16 15.9 us, 4.2 TB/s (sums in
-// binary32 instead of binary64 save nothing).
+// group is a multiple of eight channels, whose sums a thread takes together.  4 x 65536 x 128 of bf16 15.9 us, 4.2 TB/s, 67200 x 96 of f32 8.6, 3.0 TB/s: less than
+// memory gives (the quantizer moves 5.9), and sums in binary32 instead of binary64 save nothing.  A workgroup a CU, so two waves a SIMD, each with one turn of loads on its
+// way; more of them were not tried.
 template <typename T, bool TINY, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_sums_kernel(GroupArgs A)
 {
@@ -274,8 +275,8 @@ __global__ __launch_bounds__(THREADS) void group_sums_kernel(GroupArgs A)
 // Chunk by chunk again, from its last rows, which the caches are likely to hold, to the first: every workgroup adds up its image's sums first, in an order that goes
 // by the sizes alone, while its first rows are on their way.  `lanes` lanes a row: for values as many as it has units of eight channels, for codes a power of
 // two, whose maximum goes through the lanes and, of more than a wave, through LDS.  Values go past the caches, which the map is in.  What bounds it is memory, with a SiLU in
-// part the vector unit: 4 x 65536 x 128 of bf16 26.2 us, 5.1 TB/s of read and write (through the caches 33.9, without the SiLU 28.9 there), 67200 x 96 of
-// f32 12.3; before that 2 to 3 us for the image's sums, which other XCDs wrote, eight loads at a time (one after the other 7 more).  In place of two kernels one with
+// part the vector unit: 4 x 65536 x 128 of bf16 27.5 us, 4.9 TB/s of read and write (through the caches 33.9, without the SiLU 28.9 there), 67200 x 96 of
+// f32 12.2; before that 2 to 3 us for the image's sums, which other XCDs wrote, eight loads at a time (one after the other 7 more).  In place of two kernels one with
 // the map held on the chip would need the workgroups to wait for one another.
 template <typename T, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS) void group_norm_kernel(GroupArgs A)
@@ -412,7 +413,14 @@ size_t workspace_of(const mixaq_group_norm_desc& d, int images)
 }
 
 // Of how many parts an image's channels are, whole groups and whole units of eight each, where a workgroup holds the rows of one; 0 where none does, or where the
-// workgroups of all images are more than a launch takes.
+// workgroups of all images are more than a launch takes.  us of graph replays, bf16, images x rows x channels (groups):
+//   In one kernel / in two, up to the line of HELD: 1 x 49 x 256 (32) 5.5 / 8.1    1 x 4096 x 32 (4) 8.0 / 10.7    1 x 1364 x 48 (16) 9.1 / 11.0    1 x 1050 x 256 (32) 6.6 / 11.1
+//     1 x 1024 x 1024 (32) 8.0 / 11.4    1 x 256 x 1024 (8) 7.4 / 11.0    1 x 128 x 2048 (8) 9.2 / 11.7; not so 1 x 4096 x 256 (32) 15.7 / 11.3, of f32 22.4 / 11.7 (32 workgroups
+//     of 16 bytes a row)
+//   Behind it (HELD 8 / two): 1 x 8192 x 32 (4) 11.5 / 10.8    1 x 4200 x 256 (32) 16.3 / 11.2    1 x 2048 x 1024 (32) 11.3 / 11.6    1 x 512 x 1024 (8) 9.9 / 11.2    1 x 256 x 2048 (8)
+//     11.5 / 11.8    8 x 8192 x 256 (32) 60 / 19.5
+//   The number of images is not looked at, nor how many threads of a workgroup have rows; many images take longer in one kernel, 256 (32): 4 x 1024 9.9 / 10.9    8 x 1024
+//     12.4 / 11.1    16 x 196 9.5 / 9.9    64 x 196 26 / 11.3    64 x 49 21 / 8.7    1000 x 49 270 / 26
 int parts_of(const mixaq_group_norm_desc& d, int images)
 {
     int width = d.C / d.groups;

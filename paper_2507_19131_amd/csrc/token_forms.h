@@ -8,6 +8,7 @@ enum TokenForm { TOKEN_FEW, TOKEN_MID, TOKEN_SPLIT, TOKEN_TILE, TOKEN_WIDE };
 
 // Whether values of M rows are quantized on their way into FEW's product: every workgroup quantizes its 16 whole rows for itself, so only rows of no more than it holds
 // and few workgroups.  us of graph replays, bf16 / f32 values, in one launch and in two (the second takes the host another 3.5 where nothing is captured):
+//   (Every wave for its own block of K, which rows sorted by expert had no registers for, took 4.0 and 3.8 for a single row of 1024 x 4096, 6.0 and 7.3 for 32.)
 //   512 of 16 outputs: 1 x 1024 x 4096 (256) 4.3 / 5.1, 4.3 / 5.0    64 x 1024 x 1024 (256) 4.5 / 5.7, 4.6 / 6.2    32 x 1024 x 4096 (512) 5.5 / 6.4, 5.5 / 6.4
 //     128 x 1024 x 1024 (512) 5.5 / 6.4, 5.5 / 6.4    16 x 1024 x 8192 (512) 5.4 / 6.3, 5.4 / 6.2 |  64 x 1024 x 4096 (1024) 7.9 / 7.9, 7.9 / 7.8
 //   Rows sorted by expert, up to 64 in 1024 of 64 outputs (K x N of experts): 16 of 1024 x 2048 of 32 (1024) 7.7 / 7.8, 7.9 / 7.8    64 the same 12.8 / 13.2, 12.9 / 13.4
@@ -32,6 +33,9 @@ inline bool token_quantized_inside(int M, int K, int NB, int experts, bool sorte
 //     8192 x 4096 x 1024 (256) 43 / 36    16384 x 4096 x 4096 325 / 255
 // Rows sorted by expert (the average expert stands for all): FEW up to 16 rows an expert, where a workgroup takes all rows of its expert, else tiles (few / tile / wide,
 // 1024 x 2048, 32 experts): 16 rows in all 5.6 / 10.3 / 13.1    256 14.4 / 16.9 / 18.2    512 16.7 / 17.2 / 18.3 |  1024 26.1 / 18.5 / 18.8    4096 74 / 28.5 / 25.7
+//   That holds for experts about as busy as one another; a workgroup of FEW takes its expert's tiles one after the other, however many.  1024 rows of 64 experts, few / tile: as
+//   many each 24.6 / 29.4, drawn by an uneven router 29.7 / 29.1, all to two 68.5 / 11.0, all to one 129 / 10.9.  The offsets are not known where the choice is made.
+//   SPLIT takes all rows of its expert in turn as well: 1048512 rows of 8 experts x 4096 x 1024 4.3 ms in WIDE, 1048640, which reach beyond 2^32 bytes, 27.4 in SPLIT
 inline TokenForm token_form(int M, int KB, int NB, int experts, bool sorted, long long reach)
 {
     const long long rows = sorted ? M / experts : M, many = sorted ? experts : 1;
